@@ -46,6 +46,26 @@ CACNN_POOL_AVG = 0
 CACNN_POOL_MAX = 1
 
 
+CACNN_GATE_SILU = 0
+CACNN_GATE_GELU = 1
+CACNN_GATE_GELU_TANH = 2
+
+
+class QuantizeProblem(ctypes.Structure):
+    """cacnn_quantize_problem: T, C, block_rows and the row strides (0: from the tensors, or dense)."""
+    _fields_ = [(n, ctypes.c_int64) for n in ("T", "C", "block_rows", "ld_x", "ld_q")]
+
+
+class MatmulProblem(ctypes.Structure):
+    """cacnn_matmul_problem: T, C, K and the row strides (0: from the tensors, or dense)."""
+    _fields_ = [(n, ctypes.c_int64) for n in ("T", "C", "K", "ld_x", "ld_w", "ld_out")]
+
+
+class GatedProblem(ctypes.Structure):
+    """cacnn_gated_problem: T, C, F, activation and the row strides (0: from the tensors, or dense)."""
+    _fields_ = [(n, ctypes.c_int64) for n in ("T", "C", "F", "activation", "ld_x", "ld_w", "ld_out", "ld_pre", "ld_grad_x", "ld_grad_w")]
+
+
 class Machine(ctypes.Structure):
     _fields_ = [("lds_bytes", ctypes.c_int64), ("vgpr_bytes_per_cu", ctypes.c_int64), ("num_cu", ctypes.c_int64)]
 
@@ -141,6 +161,19 @@ _lib.cacnn_pool_lower_bound.argtypes = [ctypes.POINTER(Problem), ctypes.c_double
 _lib.cacnn_pool_forward.restype = ctypes.c_int
 _lib.cacnn_pool_forward.argtypes = [ctypes.POINTER(Problem), ctypes.c_int, ctypes.c_int, ctypes.c_void_p, ctypes.c_void_p,
                                     ctypes.c_void_p]
+_V = ctypes.c_void_p
+_lib.cacnn_quantize.restype = ctypes.c_int
+_lib.cacnn_quantize.argtypes = [ctypes.POINTER(QuantizeProblem), ctypes.c_int, _V, _V, _V, _V]
+_lib.cacnn_matmul_scaled.restype = ctypes.c_int
+_lib.cacnn_matmul_scaled.argtypes = [ctypes.POINTER(MatmulProblem), _V, _V, _V, _V, ctypes.c_int, _V, _V]
+_lib.cacnn_gated_forward.restype = ctypes.c_int
+_lib.cacnn_gated_forward.argtypes = [ctypes.POINTER(GatedProblem), ctypes.c_int] + [_V] * 7
+_lib.cacnn_gated_forward_scaled.restype = ctypes.c_int
+_lib.cacnn_gated_forward_scaled.argtypes = [ctypes.POINTER(GatedProblem)] + [_V] * 6 + [ctypes.c_int, _V, _V]
+_lib.cacnn_gated_workspace.restype = ctypes.c_int
+_lib.cacnn_gated_workspace.argtypes = [ctypes.POINTER(GatedProblem), ctypes.c_int, ctypes.POINTER(ctypes.c_size_t)]
+_lib.cacnn_gated_backward.restype = ctypes.c_int
+_lib.cacnn_gated_backward.argtypes = [ctypes.POINTER(GatedProblem), ctypes.c_int] + [_V] * 10 + [ctypes.c_size_t, _V]
 _lib.cacnn_probe_mfma.restype = ctypes.c_int
 _lib.cacnn_probe_mfma.argtypes = [ctypes.c_int, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int32,
                                   ctypes.POINTER(ctypes.c_int64), ctypes.c_void_p]
@@ -463,6 +496,143 @@ def cacnn_pool_forward(problem, dtype: int, mode: int, image, out, stream=None) 
                                  _stream_handle(stream))
     if rc != 0:
         raise CacnnError(rc, "cacnn_pool_forward")
+
+
+# ---- feed-forward operators: two-dimensional device tensors whose last index is contiguous; rows may lie further apart
+_FEED_DTYPE = {CACNN_F32: torch.float32, CACNN_BF16_F32ACC: torch.bfloat16}
+_BYTES = (torch.float8_e4m3fn, torch.uint8)
+
+
+def _feed_dtype(where: str, dtype):
+    if int(dtype) not in _FEED_DTYPE:
+        raise CacnnError(3, where)
+    return (_FEED_DTYPE[int(dtype)],)
+
+
+class _Feed:
+    """Checks of one call: every tensor's type, shape and layout against the problem, all on the device of `stream` (which is the current one
+    of the tensors' device where none is given).  The library trusts its pointers."""
+    def __init__(self, where, problem, kind, stream):
+        self.where, self.stream, self.device = where, stream, None
+        self.problem = kind.from_buffer_copy(problem) if isinstance(problem, kind) else kind(*[int(x) for x in problem])
+
+    def take(self, name, t, rows, cols, types, ld=None):
+        """The address of `t`, [rows][cols] of one of `types`; its row stride goes into the problem's field `ld` (None: dense rows)."""
+        if not isinstance(t, torch.Tensor):
+            raise TypeError(f"{self.where}: {name} must be a tensor")
+        if t.dtype not in types:
+            raise ValueError(f"{self.where}: {name} is {t.dtype}, the call needs {types[0]}")
+        if not t.is_cuda:
+            raise ValueError(f"{self.where} takes device tensors, {name} is on {t.device}")
+        if self.device is None:
+            self.device = t.device
+        if t.device != self.device:
+            raise ValueError(f"{self.where}: {name} is on {t.device}, the other tensors on {self.device}")
+        if tuple(t.shape) != (rows, cols):
+            raise ValueError(f"{self.where}: {name} is {tuple(t.shape)}, the problem needs {(rows, cols)}")
+        stride = t.stride(0) if rows > 1 else cols
+        if t.numel() and ((t.stride(1) != 1 and cols > 1) or stride < cols):
+            raise ValueError(f"{self.where}: {name}'s rows must be contiguous and not overlap, its strides are {t.stride()}")
+        if ld is None:
+            if t.numel() and stride != cols:
+                raise ValueError(f"{self.where}: {name} must be contiguous")
+        elif rows > 1 and t.numel():
+            said = self.strides.setdefault(ld, stride)
+            if said != stride:
+                raise ValueError(f"{self.where}: {name}'s rows lie {stride} elements apart, those of the array it goes with {said}")
+            if getattr(self.problem, ld) not in (0, stride):
+                raise ValueError(f"{self.where}: {name}'s rows lie {stride} elements apart, the problem says {getattr(self.problem, ld)}")
+            setattr(self.problem, ld, stride)
+        return t.data_ptr()
+
+    @property
+    def strides(self):
+        return self.__dict__.setdefault("_strides", {})
+
+    def call(self, function, *args):
+        stream = self.stream
+        if stream is not None and not isinstance(stream, int) and stream.device != self.device:
+            raise ValueError(f"{self.where}: the stream is on {stream.device}, the tensors on {self.device}")
+        if self.device.index != torch.cuda.current_device():
+            with torch.cuda.device(self.device):
+                rc = function(ctypes.byref(self.problem), *args, _stream_handle(stream))
+        else:
+            rc = function(ctypes.byref(self.problem), *args, _stream_handle(stream))
+        if rc != 0:
+            raise CacnnError(rc, self.where)
+
+
+def cacnn_quantize(problem, dtype: int, x, q, scale, stream=None) -> None:
+    """Enqueue the quantisation of X[T,C] to 8-bit floats Q[T,C] with a scale for each block of 128 columns and problem.block_rows (1 or 128)
+    rows, scale[ceil(T/block_rows), ceil(C/128)] fp32.  problem: QuantizeProblem or (T, C, block_rows)."""
+    f = _Feed("cacnn_quantize", problem, QuantizeProblem, stream)
+    p = f.problem
+    if p.block_rows not in (1, 128):
+        raise CacnnError(3, f.where)
+    f.call(_lib.cacnn_quantize, int(dtype), f.take("x", x, p.T, p.C, _feed_dtype(f.where, dtype), "ld_x"), f.take("q", q, p.T, p.C, _BYTES, "ld_q"),
+           f.take("scale", scale, -(-p.T // p.block_rows), -(-p.C // 128), (torch.float32,)))
+
+
+def cacnn_matmul_scaled(problem, x, x_scale, w, w_scale, out_dtype: int, out, stream=None) -> None:
+    """Enqueue Out[T,K] = X[T,C] W[K,C]' of 8-bit floats (torch.float8_e4m3fn, or their bytes) with scales x_scale[T, ceil(C/128)] and
+    w_scale[ceil(K/128), ceil(C/128)].  problem: MatmulProblem or (T, C, K)."""
+    f = _Feed("cacnn_matmul_scaled", problem, MatmulProblem, stream)
+    p = f.problem
+    blocks = -(-p.C // 128)
+    f.call(_lib.cacnn_matmul_scaled, f.take("x", x, p.T, p.C, _BYTES, "ld_x"), f.take("x_scale", x_scale, p.T, blocks, (torch.float32,)),
+           f.take("w", w, p.K, p.C, _BYTES, "ld_w"), f.take("w_scale", w_scale, -(-p.K // 128), blocks, (torch.float32,)), int(out_dtype),
+           f.take("out", out, p.T, p.K, _feed_dtype(f.where, out_dtype), "ld_out"))
+
+
+def cacnn_gated_forward(problem, dtype: int, x, w_gate, w_up, out, gate=None, up=None, stream=None) -> None:
+    """Enqueue Out[T,F] = act(X[T,C] W_gate[F,C]') * (X W_up[F,C]'), and, where tensors are given for them, the two products gate[T,F]
+    and up[T,F].  problem: GatedProblem or (T, C, F, activation)."""
+    f = _Feed("cacnn_gated_forward", problem, GatedProblem, stream)
+    p, t = f.problem, _feed_dtype("cacnn_gated_forward", dtype)
+    f.call(_lib.cacnn_gated_forward, int(dtype), f.take("x", x, p.T, p.C, t, "ld_x"), f.take("w_gate", w_gate, p.F, p.C, t, "ld_w"),
+           f.take("w_up", w_up, p.F, p.C, t, "ld_w"), f.take("out", out, p.T, p.F, t, "ld_out"),
+           None if gate is None else f.take("gate", gate, p.T, p.F, t, "ld_pre"), None if up is None else f.take("up", up, p.T, p.F, t, "ld_pre"))
+
+
+def cacnn_gated_forward_scaled(problem, x, x_scale, w_gate, w_gate_scale, w_up, w_up_scale, out_dtype: int, out, stream=None) -> None:
+    """cacnn_gated_forward of 8-bit floats with scales as for cacnn_matmul_scaled; Out in out_dtype."""
+    f = _Feed("cacnn_gated_forward_scaled", problem, GatedProblem, stream)
+    p = f.problem
+    blocks, fp32 = -(-p.C // 128), (torch.float32,)
+    f.call(_lib.cacnn_gated_forward_scaled, f.take("x", x, p.T, p.C, _BYTES, "ld_x"), f.take("x_scale", x_scale, p.T, blocks, fp32),
+           f.take("w_gate", w_gate, p.F, p.C, _BYTES, "ld_w"), f.take("w_gate_scale", w_gate_scale, -(-p.F // 128), blocks, fp32),
+           f.take("w_up", w_up, p.F, p.C, _BYTES, "ld_w"), f.take("w_up_scale", w_up_scale, -(-p.F // 128), blocks, fp32), int(out_dtype),
+           f.take("out", out, p.T, p.F, _feed_dtype(f.where, out_dtype), "ld_out"))
+
+
+def cacnn_gated_workspace(problem, dtype: int) -> int:
+    """Bytes of device memory that cacnn_gated_backward needs beside its arrays (host only)."""
+    p = problem if isinstance(problem, GatedProblem) else GatedProblem(*[int(x) for x in problem])
+    n = ctypes.c_size_t(0)
+    rc = _lib.cacnn_gated_workspace(ctypes.byref(p), int(dtype), ctypes.byref(n))
+    if rc != 0:
+        raise CacnnError(rc, "cacnn_gated_workspace")
+    return n.value
+
+
+def cacnn_gated_backward(problem, dtype: int, x, w_gate, w_up, grad_out, grad_x, grad_w_gate, grad_w_up, workspace, gate=None, up=None,
+                         stream=None) -> None:
+    """Enqueue the gradients of cacnn_gated_forward for grad_out[T,F]: grad_x[T,C] and grad_w_gate, grad_w_up[F,C] (None: not wanted).  gate and up
+    are what the forward pass kept, or None.  workspace: a contiguous tensor of at least cacnn_gated_workspace bytes, one for each call
+    that may run at the same time."""
+    f = _Feed("cacnn_gated_backward", problem, GatedProblem, stream)
+    p, t = f.problem, _feed_dtype("cacnn_gated_backward", dtype)
+
+    def optional(name, tensor, rows, cols, ld):
+        return None if tensor is None else f.take(name, tensor, rows, cols, t, ld)
+
+    args = [f.take("x", x, p.T, p.C, t, "ld_x"), f.take("w_gate", w_gate, p.F, p.C, t, "ld_w"), f.take("w_up", w_up, p.F, p.C, t, "ld_w"),
+            optional("gate", gate, p.T, p.F, "ld_pre"), optional("up", up, p.T, p.F, "ld_pre"), f.take("grad_out", grad_out, p.T, p.F, t, "ld_out"),
+            optional("grad_x", grad_x, p.T, p.C, "ld_grad_x"), optional("grad_w_gate", grad_w_gate, p.F, p.C, "ld_grad_w"),
+            optional("grad_w_up", grad_w_up, p.F, p.C, "ld_grad_w")]
+    if workspace.device != f.device or not workspace.is_contiguous():
+        raise ValueError(f"{f.where}: workspace must be a contiguous tensor on {f.device}")
+    f.call(_lib.cacnn_gated_backward, int(dtype), *args, workspace.data_ptr(), workspace.numel() * workspace.element_size())
 
 
 def cacnn_probe_mfma(dtype: int, operands, sink, iters: int, stream=None) -> int:

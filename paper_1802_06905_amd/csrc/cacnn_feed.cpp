@@ -1,0 +1,211 @@
+// Feed-forward operators, host side: checks of the arguments and what is launched.  See include/cacnn.h.
+#include <stdint.h>
+
+#include <algorithm>
+
+#include "../../include/cacnn.h"
+#include "cacnn_feed.h"
+#include "cacnn_internal.h"
+
+using namespace cacnn;
+
+namespace {
+
+// Row lengths and strides: 32-bit offsets within the 256 rows of a tile, in units of a byte, stay below 2^30
+constexpr int64_t kMostColumns = 1 << 20, kMostRows = INT32_MAX;
+// and the workgroups of a launch are at most 2^31 - 1; a tile has at least 32 rows or columns
+bool tiles_in_range(int64_t rows, int64_t cols) { return (rows + 31) / 32 * ((cols + 31) / 32) <= INT32_MAX; }
+
+bool columns(int64_t n) { return n >= 1 && n <= kMostColumns; }
+bool rows(int64_t n) { return n >= 0 && n <= kMostRows; }
+// a row stride, 0 for dense rows
+bool stride(int64_t* ld, int64_t cols) {
+    if (*ld == 0) *ld = cols;
+    return *ld >= cols && *ld <= kMostColumns;
+}
+bool multiple(const void* p, size_t of) { return reinterpret_cast<uintptr_t>(p) % of == 0; }
+bool element_type(int dtype) { return dtype == CACNN_F32 || dtype == CACNN_BF16_F32ACC; }
+
+FeedOperand operand(const void* p, int64_t ld, int size, int64_t rows, int64_t k) {
+    return {static_cast<const char*>(p), ld * size, k, rows};
+}
+// an output whose groups of four columns start at multiples of their size leaves in wide stores
+FeedOut output(void* p, int64_t ld, int size) {
+    return {static_cast<char*>(p), ld * size, size, multiple(p, 4 * size) && ld % 4 == 0};
+}
+
+int64_t padded(int64_t F) { return (F + 63) / 64 * 64; }      // columns of a row in the workspace
+
+bool valid_gated(cacnn_gated_problem* p) {
+    return rows(p->T) && columns(p->C) && columns(p->F) && stride(&p->ld_x, p->C) && stride(&p->ld_w, p->C) && stride(&p->ld_out, p->F) &&
+           stride(&p->ld_pre, p->F) && stride(&p->ld_grad_x, p->C) && stride(&p->ld_grad_w, p->C) && tiles_in_range(p->T, padded(p->F)) &&
+           tiles_in_range(p->T, p->C);
+}
+bool activation(int64_t a) { return a == CACNN_GATE_SILU || a == CACNN_GATE_GELU || a == CACNN_GATE_GELU_TANH; }
+
+int launched(int rc) { return rc == 0 ? CACNN_OK : CACNN_ERR_LAUNCH; }
+
+}  // namespace
+
+extern "C" {
+
+int cacnn_quantize(const cacnn_quantize_problem* problem, int dtype, const void* x, void* q, float* scale, void* hip_stream) {
+    if (!problem || (problem->T != 0 && (!x || !q || !scale))) return CACNN_ERR_NULL;
+    cacnn_quantize_problem p = *problem;
+    if (!element_type(dtype) || (p.block_rows != 1 && p.block_rows != kScaleBlock)) return CACNN_ERR_UNSUPPORTED;
+    if (!rows(p.T) || !columns(p.C) || !stride(&p.ld_x, p.C) || !stride(&p.ld_q, p.C)) return CACNN_ERR_INVALID_ARG;
+    const int size = feed_size(dtype);
+    if (!multiple(x, size) || !multiple(scale, 4)) return CACNN_ERR_INVALID_ARG;
+    if (!device_present()) return CACNN_ERR_NO_DEVICE;
+    if (p.T == 0) return CACNN_OK;
+    QuantizeArgs a = {};
+    a.x = static_cast<const char*>(x), a.ld_x = p.ld_x * size;
+    a.q = static_cast<uint8_t*>(q), a.ld_q = p.ld_q, a.scale = scale;
+    a.T = p.T, a.C = p.C;
+    a.blocks = (int32_t)((p.C + kScaleBlock - 1) / kScaleBlock);
+    a.wide = multiple(x, 16) && a.ld_x % 16 == 0 && multiple(q, 8) && p.ld_q % 8 == 0;
+    return launched(launch_quantize(a, dtype, (int)p.block_rows, hip_stream));
+}
+
+int cacnn_matmul_scaled(const cacnn_matmul_problem* problem, const void* x, const float* x_scale, const void* w, const float* w_scale, int out_dtype,
+                        void* out, void* hip_stream) {
+    if (!problem || !w || !w_scale || (problem->T != 0 && (!x || !x_scale || !out))) return CACNN_ERR_NULL;
+    if (!element_type(out_dtype)) return CACNN_ERR_UNSUPPORTED;
+    cacnn_matmul_problem p = *problem;
+    if (!rows(p.T) || !columns(p.C) || !columns(p.K) || !stride(&p.ld_x, p.C) || !stride(&p.ld_w, p.C) || !stride(&p.ld_out, p.K) ||
+        !tiles_in_range(p.T, p.K))
+        return CACNN_ERR_INVALID_ARG;
+    const int size = feed_size(out_dtype);
+    if (!multiple(x_scale, 4) || !multiple(w_scale, 4) || !multiple(out, size)) return CACNN_ERR_INVALID_ARG;
+    if (!device_present()) return CACNN_ERR_NO_DEVICE;
+    if (p.T == 0) return CACNN_OK;
+    FeedArgs a = {};
+    a.segments = a.products = 1;
+    a.q[0] = operand(x, p.ld_x, 1, p.T, p.C);
+    a.p[0] = operand(w, p.ld_w, 1, p.K, p.C);
+    a.out[0] = output(out, p.ld_out, size);
+    a.M = p.T, a.N = p.K;
+    a.q_scale = x_scale, a.p_scale[0] = w_scale;
+    a.scale_cols = (int32_t)((p.C + kScaleBlock - 1) / kScaleBlock);
+    return launched(launch_matmul(a, FEED_PLAIN, FEED_E4M3, hip_stream));
+}
+
+int cacnn_gated_forward(const cacnn_gated_problem* problem, int dtype, const void* x, const void* w_gate, const void* w_up, void* out, void* gate,
+                        void* up, void* hip_stream) {
+    if (!problem || !w_gate || !w_up || (problem->T != 0 && (!x || !out))) return CACNN_ERR_NULL;
+    cacnn_gated_problem p = *problem;
+    if (!element_type(dtype) || !activation(p.activation)) return CACNN_ERR_UNSUPPORTED;
+    if (!valid_gated(&p) || (p.T != 0 && !gate != !up)) return CACNN_ERR_INVALID_ARG;
+    const int size = feed_size(dtype);
+    if (!multiple(x, size) || !multiple(w_gate, size) || !multiple(w_up, size) || !multiple(out, size) || !multiple(gate, size) || !multiple(up, size))
+        return CACNN_ERR_INVALID_ARG;
+    if (!device_present()) return CACNN_ERR_NO_DEVICE;
+    if (p.T == 0) return CACNN_OK;
+    FeedArgs a = {};
+    a.segments = a.products = 1;
+    a.q[0] = operand(x, p.ld_x, size, p.T, p.C);
+    a.p[0] = operand(w_gate, p.ld_w, size, p.F, p.C);
+    a.p[1] = operand(w_up, p.ld_w, size, p.F, p.C);
+    a.out[0] = output(out, p.ld_out, size);
+    if (gate) a.gate_out = output(gate, p.ld_pre, size), a.up_out = output(up, p.ld_pre, size);
+    a.M = p.T, a.N = p.F;
+    a.activation = (int32_t)p.activation;
+    return launched(launch_matmul(a, FEED_GATED, dtype, hip_stream));
+}
+
+int cacnn_gated_forward_scaled(const cacnn_gated_problem* problem, const void* x, const float* x_scale, const void* w_gate, const float* w_gate_scale,
+                               const void* w_up, const float* w_up_scale, int out_dtype, void* out, void* hip_stream) {
+    if (!problem || !w_gate || !w_gate_scale || !w_up || !w_up_scale || (problem->T != 0 && (!x || !x_scale || !out))) return CACNN_ERR_NULL;
+    cacnn_gated_problem p = *problem;
+    if (!element_type(out_dtype) || !activation(p.activation)) return CACNN_ERR_UNSUPPORTED;
+    if (!valid_gated(&p)) return CACNN_ERR_INVALID_ARG;
+    const int size = feed_size(out_dtype);
+    if (!multiple(x_scale, 4) || !multiple(w_gate_scale, 4) || !multiple(w_up_scale, 4) || !multiple(out, size)) return CACNN_ERR_INVALID_ARG;
+    if (!device_present()) return CACNN_ERR_NO_DEVICE;
+    if (p.T == 0) return CACNN_OK;
+    FeedArgs a = {};
+    a.segments = a.products = 1;
+    a.q[0] = operand(x, p.ld_x, 1, p.T, p.C);
+    a.p[0] = operand(w_gate, p.ld_w, 1, p.F, p.C);
+    a.p[1] = operand(w_up, p.ld_w, 1, p.F, p.C);
+    a.out[0] = output(out, p.ld_out, size);
+    a.M = p.T, a.N = p.F;
+    a.q_scale = x_scale, a.p_scale[0] = w_gate_scale, a.p_scale[1] = w_up_scale;
+    a.scale_cols = (int32_t)((p.C + kScaleBlock - 1) / kScaleBlock);
+    a.activation = (int32_t)p.activation;
+    return launched(launch_matmul(a, FEED_GATED, FEED_E4M3, hip_stream));
+}
+
+int cacnn_gated_workspace(const cacnn_gated_problem* problem, int dtype, size_t* bytes) {
+    if (!problem || !bytes) return CACNN_ERR_NULL;
+    cacnn_gated_problem p = *problem;
+    if (!element_type(dtype) || !activation(p.activation)) return CACNN_ERR_UNSUPPORTED;
+    if (!valid_gated(&p)) return CACNN_ERR_INVALID_ARG;
+    *bytes = (size_t)(2 * p.T * padded(p.F)) * feed_size(dtype);
+    return CACNN_OK;
+}
+
+int cacnn_gated_backward(const cacnn_gated_problem* problem, int dtype, const void* x, const void* w_gate, const void* w_up, const void* gate,
+                         const void* up, const void* grad_out, void* grad_x, void* grad_w_gate, void* grad_w_up, void* workspace,
+                         size_t workspace_bytes, void* hip_stream) {
+    if (!problem || !w_gate || !w_up || (problem->T != 0 && (!x || !grad_out || !workspace))) return CACNN_ERR_NULL;
+    cacnn_gated_problem p = *problem;
+    if (!element_type(dtype) || !activation(p.activation)) return CACNN_ERR_UNSUPPORTED;
+    if (!valid_gated(&p) || (p.T != 0 && !gate != !up) || !grad_w_gate != !grad_w_up || (p.T != 0 && !grad_x && !grad_w_gate))
+        return CACNN_ERR_INVALID_ARG;
+    const int size = feed_size(dtype);
+    for (const void* q : {x, w_gate, w_up, gate, up, grad_out, (const void*)grad_x, (const void*)grad_w_gate, (const void*)grad_w_up})
+        if (!multiple(q, size)) return CACNN_ERR_INVALID_ARG;
+    const int64_t ld = padded(p.F);
+    if (!multiple(workspace, 16) || workspace_bytes / size / 2 < (size_t)(p.T * ld)) return CACNN_ERR_INVALID_ARG;
+    if (!device_present()) return CACNN_ERR_NO_DEVICE;
+    // the gradients of the two products, in the workspace with rows padded by zeros
+    char* const grad_gate = static_cast<char*>(workspace);
+    char* const grad_up = grad_gate + p.T * ld * size;
+    if (p.T != 0) {
+        if (gate) {
+            GateArgs a = {};
+            a.gate = static_cast<const char*>(gate), a.up = static_cast<const char*>(up), a.grad_out = static_cast<const char*>(grad_out);
+            a.ld_pre = p.ld_pre * size, a.ld_out = p.ld_out * size;
+            a.grad_gate = grad_gate, a.grad_up = grad_up, a.ld = ld * size;
+            a.T = p.T, a.F = p.F, a.cols = ld;
+            a.activation = (int32_t)p.activation;
+            a.wide = multiple(gate, 16) && multiple(up, 16) && multiple(grad_out, 16) && a.ld_pre % 16 == 0 && a.ld_out % 16 == 0;
+            if (launch_gate_grad(a, dtype, hip_stream) != 0) return CACNN_ERR_LAUNCH;
+        } else {
+            FeedArgs a = {};
+            a.segments = a.products = 1;
+            a.q[0] = operand(x, p.ld_x, size, p.T, p.C);
+            a.p[0] = operand(w_gate, p.ld_w, size, p.F, p.C);
+            a.p[1] = operand(w_up, p.ld_w, size, p.F, p.C);
+            a.out[0] = output(grad_gate, ld, size), a.out[1] = output(grad_up, ld, size);
+            a.M = p.T, a.N = p.F;
+            a.activation = (int32_t)p.activation;
+            a.grad_out = static_cast<const char*>(grad_out), a.grad_out_ld = p.ld_out * size;
+            a.grad_out_wide = multiple(grad_out, 4 * size) && p.ld_out % 4 == 0;
+            a.grad_cols = (int32_t)ld;
+            if (launch_matmul(a, FEED_GATED, dtype, hip_stream) != 0) return CACNN_ERR_LAUNCH;
+        }
+    }
+    if (grad_x && p.T != 0) {
+        FeedArgs a = {};
+        a.segments = 2, a.products = 1;
+        a.q[0] = operand(grad_gate, ld, size, p.T, p.F), a.q[1] = operand(grad_up, ld, size, p.T, p.F);
+        a.p[0] = operand(w_gate, p.ld_w, size, p.C, p.F), a.p[1] = operand(w_up, p.ld_w, size, p.C, p.F);
+        a.out[0] = output(grad_x, p.ld_grad_x, size);
+        a.M = p.T, a.N = p.C;
+        if (launch_matmul(a, FEED_RIGHT, dtype, hip_stream) != 0) return CACNN_ERR_LAUNCH;
+    }
+    if (grad_w_gate) {
+        FeedArgs a = {};
+        a.segments = 1, a.products = 2;
+        a.q[0] = operand(grad_gate, ld, size, p.F, p.T), a.q[1] = operand(grad_up, ld, size, p.F, p.T);
+        a.p[0] = operand(x, p.ld_x, size, p.C, p.T);
+        a.out[0] = output(grad_w_gate, p.ld_grad_w, size), a.out[1] = output(grad_w_up, p.ld_grad_w, size);
+        a.M = p.F, a.N = p.C;
+        if (launch_matmul(a, FEED_BOTH, dtype, hip_stream) != 0) return CACNN_ERR_LAUNCH;
+    }
+    return CACNN_OK;
+}
+
+}  // extern "C"

@@ -1,0 +1,93 @@
+// Interface between the host side of the feed-forward operators (cacnn_feed.cpp) and their kernels (cacnn_matmul.hip, cacnn_feed.hip).
+// Not part of the public ABI.
+#ifndef CACNN_FEED_H
+#define CACNN_FEED_H
+
+#include <stddef.h>
+#include <stdint.h>
+
+namespace cacnn {
+
+// Element types of the operands as the kernels know them; the first two are cacnn_dtype's.
+// 8 bits twice: multiplied by the 8-bit matrix instructions, or turned into bf16 (which holds them exactly) and multiplied by those of bf16.  The
+// 8-bit instructions, with or without scales, the ones with 16 indices as well, add the products of eight adjacent contraction indices
+// with the bits below 2^-13 of the largest's power of two cut off (measured with single products; sums of such groups and the accumulator are
+// fp32): 5e-5 of a random sum of 64 products, against 4e-8 with bf16's.  That is far below the rounding of a bf16 result, and far above that of an
+// fp32 one: results in bf16 are computed by the former, which are twice as fast, fp32 results by the latter.
+enum { FEED_F32 = 0, FEED_BF16 = 1, FEED_E4M3 = 2, FEED_E4M3_EXACT = 3 };
+constexpr int feed_size(int dtype) { return dtype == FEED_F32 ? 4 : dtype == FEED_BF16 ? 2 : 1; }
+
+constexpr int kScaleBlock = 128;   // elements of the contraction (and rows of a weight) that share a scale
+
+// One operand of a product: `rows` rows (of the product's output, or columns), a contraction of `k` elements.
+//   contraction contiguous: row r starts at base + r * ld bytes, its k elements follow
+//   contraction strided:    contraction index i starts at base + i * ld bytes, its `rows` elements follow
+struct FeedOperand {
+    const char* base;
+    int64_t ld;      // bytes
+    int64_t k;
+    int64_t rows;
+};
+
+// An output array of rows x cols elements of `size` bytes; wide: a lane's four columns leave in one store where all four exist
+struct FeedOut {
+    char* base;
+    int64_t ld;      // bytes
+    int32_t size;
+    int32_t wide;
+};
+
+// Which product: the contraction is contiguous in both operands and the columns come in pairs (gated), in both (plain), in the
+// rows' operand alone (right), in neither (both strided)
+enum { FEED_GATED = 0, FEED_PLAIN = 1, FEED_RIGHT = 2, FEED_BOTH = 3 };
+
+struct FeedArgs {
+    FeedOperand q[2], p[2];    // rows' and columns' operands.  gated: p = gate and up; right: two segments of the contraction; both: two products
+    FeedOut out[2];
+    int32_t segments;          // right: 2, of q[s] and p[s]; else 1
+    int32_t products;          // both: 2, of q[i] into out[i], with p[0]; else 1
+    int64_t M, N;              // rows and columns of an output
+    int32_t tiles_m, tiles_n;  // of one product
+    int32_t n_tiles;
+    // 8-bit operands: a scale for each row and 128 elements of the contraction of q, one for each 128 rows and 128 elements of p
+    const float* q_scale;
+    const float* p_scale[2];
+    int32_t scale_cols;
+    // gated: the activation; out[0] = act(gate) * up.  kept: gate and up in out[1] and up_out too.
+    // grad (grad_out set): out[0] and out[1] are the gradients of gate and up, written up to column grad_cols with zeros
+    int32_t activation;
+    FeedOut up_out;
+    FeedOut gate_out;
+    const char* grad_out;
+    int64_t grad_out_ld;       // bytes
+    int32_t grad_out_wide;
+    int32_t grad_cols;
+};
+
+// Launches the product; form, dtype as above.  0, or 1 where the runtime refused.
+int launch_matmul(const FeedArgs& a, int form, int dtype, void* stream);
+
+struct GateArgs {
+    const char *gate, *up, *grad_out;
+    int64_t ld_pre, ld_out;    // bytes
+    char *grad_gate, *grad_up;
+    int64_t ld;                // bytes
+    int64_t T, F, cols;        // cols: columns written, zeros from F on
+    int32_t activation, wide;  // wide: 16-byte loads
+};
+int launch_gate_grad(const GateArgs& a, int dtype, void* stream);
+
+struct QuantizeArgs {
+    const char* x;
+    int64_t ld_x;              // bytes
+    uint8_t* q;
+    int64_t ld_q;
+    float* scale;
+    int64_t T, C;
+    int32_t blocks;            // of 128 columns
+    int32_t wide;              // rows of x and q start at multiples of 16 and 8 bytes
+};
+int launch_quantize(const QuantizeArgs& a, int dtype, int block_rows, void* stream);
+
+}  // namespace cacnn
+#endif

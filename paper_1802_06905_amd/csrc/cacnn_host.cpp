@@ -1618,6 +1618,8 @@ int route(const cacnn_problem& p, int dtype, const void* image, const void* filt
 
 }  // namespace
 
+bool cacnn::device_present() { return have_device(); }
+
 extern "C" {
 
 int cacnn_lower_bound(const cacnn_problem* problem, double M_words, cacnn_bound* out) {

@@ -28,6 +28,9 @@ struct OncePerDevice {
     }
 };
 
+// Whether the process has a GPU (asked once).
+bool device_present();
+
 // Division of small unsigned numbers by a run-time constant with one multiply-high.
 // Exact for n * d < 2^32 (the staged-tile indices it is used on are bounded by the LDS size).
 struct FastDiv {
