@@ -26,8 +26,8 @@ bool stride(int64_t* ld, int64_t cols) {
 bool multiple(const void* p, size_t of) { return reinterpret_cast<uintptr_t>(p) % of == 0; }
 bool element_type(int dtype) { return dtype == CACNN_F32 || dtype == CACNN_BF16_F32ACC; }
 
-FeedOperand operand(const void* p, int64_t ld, int size, int64_t rows, int64_t k) {
-    return {static_cast<const char*>(p), ld * size, k, rows};
+FeedOperand operand(const void* p, int64_t ld, int size, int64_t rows, int64_t k, bool padded = false) {
+    return {static_cast<const char*>(p), ld * size, k, rows, padded};
 }
 // an output whose groups of four columns start at multiples of their size leaves in wide stores
 FeedOut output(void* p, int64_t ld, int size) {
@@ -190,7 +190,7 @@ int cacnn_gated_backward(const cacnn_gated_problem* problem, int dtype, const vo
     if (grad_x && p.T != 0) {
         FeedArgs a = {};
         a.segments = 2, a.products = 1;
-        a.q[0] = operand(grad_gate, ld, size, p.T, p.F), a.q[1] = operand(grad_up, ld, size, p.T, p.F);
+        a.q[0] = operand(grad_gate, ld, size, p.T, p.F, true), a.q[1] = operand(grad_up, ld, size, p.T, p.F, true);
         a.p[0] = operand(w_gate, p.ld_w, size, p.C, p.F), a.p[1] = operand(w_up, p.ld_w, size, p.C, p.F);
         a.out[0] = output(grad_x, p.ld_grad_x, size);
         a.M = p.T, a.N = p.C;
@@ -199,7 +199,7 @@ int cacnn_gated_backward(const cacnn_gated_problem* problem, int dtype, const vo
     if (grad_w_gate) {
         FeedArgs a = {};
         a.segments = 1, a.products = 2;
-        a.q[0] = operand(grad_gate, ld, size, p.F, p.T), a.q[1] = operand(grad_up, ld, size, p.F, p.T);
+        a.q[0] = operand(grad_gate, ld, size, p.F, p.T, true), a.q[1] = operand(grad_up, ld, size, p.F, p.T, true);
         a.p[0] = operand(x, p.ld_x, size, p.C, p.T);
         a.out[0] = output(grad_w_gate, p.ld_grad_w, size), a.out[1] = output(grad_w_up, p.ld_grad_w, size);
         a.M = p.F, a.N = p.C;

@@ -27,6 +27,7 @@ struct FeedOperand {
     int64_t ld;      // bytes
     int64_t k;
     int64_t rows;
+    bool padded;     // zeros follow each row's elements up to a multiple of 16 bytes
 };
 
 // An output array of rows x cols elements of `size` bytes; wide: a lane's four columns leave in one store where all four exist

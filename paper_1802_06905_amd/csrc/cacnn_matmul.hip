@@ -18,6 +18,7 @@
 #include "cacnn_feed.h"
 #include "cacnn_gate.h"
 #include "cacnn_internal.h"
+#include "cacnn_lds_load.h"
 
 namespace cacnn {
 
@@ -117,6 +118,93 @@ struct RegisterLoader {
 #pragma unroll
         for (int i = 0; i < Map::N; ++i) *(mu32x4*)(slab + (i * WAVES + wave) * 1024 + lane * 16) = r[i];
     }
+};
+
+// Brings slabs straight to LDS: rows and their parts are whole 16 bytes at multiples of 16 (or zeros follow them there).  Offsets beyond the operand are
+// turned into ones beyond the descriptor's bytes, which are at most 2^30: the load puts zeros there.
+constexpr uint32_t kOutside = 0x40000000u;
+__device__ __forceinline__ i32x4 bytes_from(const char* p, int64_t bytes) {
+    const uint64_t a = (uint64_t)p;
+    i32x4 d;
+    d[0] = __builtin_amdgcn_readfirstlane((int)(uint32_t)a);
+    d[1] = __builtin_amdgcn_readfirstlane((int)(uint32_t)(a >> 32) & 0xffff);
+    d[2] = __builtin_amdgcn_readfirstlane((int)bytes);
+    d[3] = 0x00020000;
+    return d;
+}
+template <int ESZ, bool STRIDED, int ROWS, int WAVES>
+struct DirectLoader {
+    using Map = SlabMap<ESZ, STRIDED, ROWS, WAVES>;
+    const char* base;
+    int64_t ld, k;
+    int bytes;                     // contiguous: of a row; strided: of a row of the tile; whole pieces of 16
+    int byte, wave;
+    i32x4 d;
+    uint32_t off[Map::N];
+
+    __device__ __forceinline__ void init(const FeedOperand& o, int64_t row0, int wave_, int lane) {
+        wave = wave_, ld = o.ld, k = o.k;
+        const int rows = (int)max((int64_t)0, min((int64_t)ROWS, o.rows - row0));
+        base = o.base + (STRIDED ? row0 * ESZ : row0 * ld);
+        if constexpr (STRIDED) {
+            bytes = (rows * ESZ + 15) & ~15;
+#pragma unroll
+            for (int i = 0; i < Map::N; ++i) {
+                const int col = Map::column(i, wave, lane);
+                off[i] = col < bytes ? (uint32_t)Map::index(i, wave, lane) * (uint32_t)ld + col : kOutside;
+            }
+        } else {
+            bytes = (int)((k * ESZ + 15) & ~15);
+            byte = Map::byte(lane);
+            d = bytes_from(base, rows ? (int64_t)(rows - 1) * ld + bytes : 0);
+#pragma unroll
+            for (int i = 0; i < Map::N; ++i) {
+                const int row = Map::row(i, wave, lane);
+                off[i] = row < rows ? (uint32_t)row * (uint32_t)ld + byte : kOutside;
+            }
+        }
+    }
+    // another array of the same shape
+    __device__ __forceinline__ void move(const FeedOperand& o, int64_t row0) {
+        base = o.base + (STRIDED ? row0 * ESZ : row0 * ld);
+        if constexpr (!STRIDED) d = bytes_from(base, (uint32_t)d[2]);
+    }
+    // slab s (none if !any: zeros) to LDS bytes `slab`
+    __device__ __forceinline__ void issue(int s, bool any, uint32_t slab) {
+        uint32_t more = 0;
+        if constexpr (STRIDED) {
+            const int64_t at = (int64_t)s * Map::KR;
+            const int64_t left = any ? min(k - at, (int64_t)Map::KR) : 0;
+            d = bytes_from(base + at * ld, left > 0 ? (left - 1) * ld + bytes : 0);
+        } else {
+            more = any && s * kSlab + byte < bytes ? s * kSlab : kOutside;
+        }
+#pragma unroll
+        for (int i = 0; i < Map::N; ++i) load_to_lds_unseen(d, off[i] + more, slab + (i * WAVES + wave) * 1024);
+    }
+};
+__device__ __forceinline__ void loads_done() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+__device__ __forceinline__ void lds_done() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
+
+// One operand's way to LDS
+template <int ESZ, bool STRIDED, int ROWS, int WAVES, bool DIRECT>
+struct Loader {
+    static constexpr bool direct = DIRECT;
+    DirectLoader<ESZ, STRIDED, ROWS, WAVES> l;
+    __device__ __forceinline__ void init(const FeedOperand& o, int64_t row0, int wave, int lane) { l.init(o, row0, wave, lane); }
+    __device__ __forceinline__ void move(const FeedOperand& o, int64_t row0) { l.move(o, row0); }
+    // begins to bring slab s, to `slab`: now, or with put() after the loads have come
+    __device__ __forceinline__ void begin(int s, bool any, char* slab) { l.issue(s, any, (uint32_t)(uintptr_t)(MAT_LDS(char)*)slab); }
+    __device__ __forceinline__ void put(char*) {}
+};
+template <int ESZ, bool STRIDED, int ROWS, int WAVES>
+struct Loader<ESZ, STRIDED, ROWS, WAVES, false> {
+    static constexpr bool direct = false;
+    RegisterLoader<ESZ, STRIDED, ROWS, WAVES> l;
+    __device__ __forceinline__ void init(const FeedOperand& o, int64_t row0, int wave, int lane) { l.init(o, row0, wave, lane); }
+    __device__ __forceinline__ void move(const FeedOperand& o, int64_t row0) { l.base = o.base + (STRIDED ? row0 * ESZ : row0 * l.ld); }
+    __device__ __forceinline__ void begin(int s, bool any, char*) { l.load(s, any); }
+    __device__ __forceinline__ void put(char* slab) { l.put(slab); }
 };
 
 // A block of 32 rows (or columns) of step `st` of a slab, as the matrix instructions take it: 16 bytes a lane
@@ -262,8 +350,9 @@ struct BlockShape {
     static constexpr int STAGE = Q_BYTES + P_BYTES + SCALES, LDS = 2 * STAGE;
 };
 
-template <int DT, int FORM, int QB, int PB, int WM, int WN>
-__global__ void __launch_bounds__(WM* WN * 64) matmul_block_kernel(const FeedArgs a) {
+// QD, PD: whether the operands go straight to LDS.
+template <int DT, int FORM, int QB, int PB, int WM, int WN, bool QD, bool PD>
+__global__ void __launch_bounds__(WM* WN * 64, WM* WN == 4 ? 2 : 1) matmul_block_kernel(const FeedArgs a) {
     using S = BlockShape<DT, FORM, QB, PB, WM, WN>;
     constexpr int ESZ = S::ESZ, WAVES = S::WAVES, KE = kSlab / ESZ;
     extern __shared__ __align__(16) char s_mem[];
@@ -272,22 +361,27 @@ __global__ void __launch_bounds__(WM* WN * 64) matmul_block_kernel(const FeedArg
     const TilePlace at = tile_place(a, blockIdx.x);
     const int64_t m0 = (int64_t)at.m * S::BM, n0 = (int64_t)at.n * S::COLS;
 
-    RegisterLoader<ESZ, S::Q_STRIDED, S::BM, WAVES> q;
-    RegisterLoader<ESZ, S::P_STRIDED, S::P_ROWS, WAVES> p[S::P_PARTS];
-    const int64_t k = a.q[0].k;
-    const int per_segment = (int)((k + KE - 1) / KE), slabs = max(1, per_segment * a.segments);
-    float row_scale = 0.f;
-    auto load = [&](int s) {
-        int of = at.product, i = s;
-        if (FORM == FEED_RIGHT && s >= per_segment && a.segments > 1) of = 1, i = s - per_segment;
-        const bool any = i < per_segment;
-        q.init(a.q[of], m0, wave, lane);
-        q.load(i, any);
+    Loader<ESZ, S::Q_STRIDED, S::BM, WAVES, QD> q;
+    Loader<ESZ, S::P_STRIDED, S::P_ROWS, WAVES, PD> p[S::P_PARTS];
+    q.init(a.q[at.product], m0, wave, lane);
 #pragma unroll
-        for (int h = 0; h < S::P_PARTS; ++h) {
-            p[h].init(a.p[S::GATED ? h : FORM == FEED_RIGHT ? of : 0], n0, wave, lane);
-            p[h].load(i, any);
-        }
+    for (int h = 0; h < S::P_PARTS; ++h) p[h].init(a.p[h], n0, wave, lane);
+    const int per_segment = (int)((a.q[0].k + KE - 1) / KE), slabs = max(1, per_segment * a.segments);
+    float row_scale = 0.f;
+    // Slab s on its way to its half of LDS, and there
+    auto begin = [&](int s) {
+        char* const stage = s_mem + (s & 1) * S::STAGE;
+        int i = s;
+        if constexpr (FORM == FEED_RIGHT)
+            if (s >= per_segment && a.segments > 1) {
+                i = s - per_segment;
+                q.move(a.q[1], m0);
+                p[0].move(a.p[1], n0);
+            }
+        const bool any = i < per_segment;
+        q.begin(i, any, stage);
+#pragma unroll
+        for (int h = 0; h < S::P_PARTS; ++h) p[h].begin(i, any, stage + S::Q_BYTES + h * S::P_ROWS * kSlab);
         if constexpr (ESZ == 1)
             if ((int)threadIdx.x < S::BM && any && m0 + threadIdx.x < a.M) row_scale = a.q_scale[(m0 + threadIdx.x) * a.scale_cols + i];
     };
@@ -302,6 +396,17 @@ __global__ void __launch_bounds__(WM* WN * 64) matmul_block_kernel(const FeedArg
     // a wave's i-th block of columns: part of p, block within it
     auto part_of = [&](int i) { return S::GATED ? i / (PB / 2) : 0; };
     auto block_of = [&](int i) { return S::GATED ? wn * (PB / 2) + i % (PB / 2) : wn * PB + i; };
+    auto q_slab = [&](int s) -> const char* { return s_mem + (s & 1) * S::STAGE; };
+    auto p_slab = [&](int s, int i) -> const char* { return s_mem + (s & 1) * S::STAGE + S::Q_BYTES + part_of(i) * S::P_ROWS * kSlab; };
+    // This wave has read what it needs of slab s - 1, and slab s is there for all; the buffer of slab s - 1 takes slab s + 1
+    auto next = [&](int s) {
+        loads_done();
+        put(s);
+        lds_done();
+        __builtin_amdgcn_s_barrier();
+        if (s + 1 < slabs) begin(s + 1);
+        asm volatile("" ::: "memory");
+    };
 
     mf32x16 acc[PB][QB];
 #pragma unroll
@@ -311,23 +416,41 @@ __global__ void __launch_bounds__(WM* WN * 64) matmul_block_kernel(const FeedArg
 #pragma unroll
             for (int v = 0; v < 16; ++v) acc[i][h][v] = 0.f;
 
-    auto compute = [&](int s) {
-        const char* const qs = s_mem + (s & 1) * S::STAGE;
-        const char* const ps = qs + S::Q_BYTES;
-        if constexpr (ESZ > 1) {
+    begin(0);
+    next(0);
+    if constexpr (ESZ > 1) {
+        // The operands of a step are read under the products of the step before, across slabs too
+        mu32x4 pv[2][PB], qv[2][QB];
+        auto read = [&](int s, int st, int set) {
 #pragma unroll
-            for (int st = 0; st < 4; ++st) {
-                mu32x4 pv[PB], qv[QB];
+            for (int i = 0; i < PB; ++i) pv[set][i] = read_block<ESZ, S::P_STRIDED, S::P_ROWS>(p_slab(s, i), block_of(i), st, lane);
 #pragma unroll
-                for (int i = 0; i < PB; ++i) pv[i] = read_block<ESZ, S::P_STRIDED, S::P_ROWS>(ps + part_of(i) * S::P_ROWS * kSlab, block_of(i), st, lane);
+            for (int h = 0; h < QB; ++h) qv[set][h] = read_block<ESZ, S::Q_STRIDED, S::BM>(q_slab(s), wm * QB + h, st, lane);
+            __builtin_amdgcn_sched_barrier(0);
+        };
+        auto products = [&](int set) {
 #pragma unroll
-                for (int h = 0; h < QB; ++h) qv[h] = read_block<ESZ, S::Q_STRIDED, S::BM>(qs, wm * QB + h, st, lane);
+            for (int i = 0; i < PB; ++i)
 #pragma unroll
-                for (int i = 0; i < PB; ++i)
-#pragma unroll
-                    for (int h = 0; h < QB; ++h) multiply<DT>(acc[i][h], pv[i], qv[h]);
+                for (int h = 0; h < QB; ++h) multiply<DT>(acc[i][h], pv[set][i], qv[set][h]);
+            __builtin_amdgcn_sched_barrier(0);
+        };
+        read(0, 0, 0);
+        for (int s = 0; s < slabs; ++s) {
+            read(s, 1, 1);
+            products(0);
+            read(s, 2, 0);
+            products(1);
+            read(s, 3, 1);
+            products(0);
+            if (s + 1 < slabs) {
+                next(s + 1);
+                read(s + 1, 0, 0);
             }
-        } else {
+            products(1);
+        }
+    } else {
+        for (int s = 0; s < slabs; ++s) {
             // a slab is one block of the scales: its sum of products first, then the product of the two scales times it
             float sp[PB], sq[QB];
 #pragma unroll
@@ -336,31 +459,38 @@ __global__ void __launch_bounds__(WM* WN * 64) matmul_block_kernel(const FeedArg
                 sp[i] = ((MAT_CONST(float)*)(uintptr_t)a.p_scale[part_of(i)])[col / kScaleBlock * a.scale_cols + s];
             }
 #pragma unroll
-            for (int h = 0; h < QB; ++h) sq[h] = *(const float*)(ps + S::P_BYTES + ((wm * QB + h) * 32 + j) * 4);
+            for (int h = 0; h < QB; ++h) sq[h] = *(const float*)(q_slab(s) + S::Q_BYTES + S::P_BYTES + ((wm * QB + h) * 32 + j) * 4);
             auto add = [&](int i, int h, const mf32x16& c) {
                 const float f = sp[i] * sq[h];
 #pragma unroll
                 for (int v = 0; v < 16; ++v) acc[i][h][v] = __builtin_fmaf(c[v], f, acc[i][h][v]);
             };
             if constexpr (DT == FEED_E4M3) {
-                mu32x4 pv[PB][2][2];
+                mu32x4 pv[PB][2][2], qv[2][2];
+                auto read_q = [&](int h) {
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) qv[x / 2][x % 2] = read_block<1, false, S::BM>(q_slab(s), wm * QB + h, x, lane);
+                };
 #pragma unroll
                 for (int i = 0; i < PB; ++i)
 #pragma unroll
-                    for (int x = 0; x < 4; ++x)
-                        pv[i][x / 2][x % 2] = read_block<1, false, S::P_ROWS>(ps + part_of(i) * S::P_ROWS * kSlab, block_of(i), x, lane);
+                    for (int x = 0; x < 4; ++x) pv[i][x / 2][x % 2] = read_block<1, false, S::P_ROWS>(p_slab(s, i), block_of(i), x, lane);
+                read_q(0);
 #pragma unroll
                 for (int h = 0; h < QB; ++h) {
-                    mu32x4 qv[2][2];
-#pragma unroll
-                    for (int x = 0; x < 4; ++x) qv[x / 2][x % 2] = read_block<1, false, S::BM>(qs, wm * QB + h, x, lane);
+                    mf32x16 c[PB];
 #pragma unroll
                     for (int i = 0; i < PB; ++i) {
-                        mf32x16 c;
 #pragma unroll
-                        for (int v = 0; v < 16; ++v) c[v] = 0.f;
-                        add(i, h, multiply_e4m3(multiply_e4m3(c, pv[i][0], qv[0]), pv[i][1], qv[1]));
+                        for (int v = 0; v < 16; ++v) c[i][v] = 0.f;
+                        c[i] = multiply_e4m3(multiply_e4m3(c[i], pv[i][0], qv[0]), pv[i][1], qv[1]);
                     }
+                    __builtin_amdgcn_sched_barrier(0);
+                    if (h + 1 < QB) read_q(h + 1);
+                    else if (s + 1 < slabs) next(s + 1);
+                    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                    for (int i = 0; i < PB; ++i) add(i, h, c[i]);
                 }
             } else {
                 mf32x16 c[PB][QB];
@@ -374,9 +504,9 @@ __global__ void __launch_bounds__(WM* WN * 64) matmul_block_kernel(const FeedArg
                 for (int x = 0; x < 4; ++x) {
                     mu32x4 pv[PB], qv[QB];
 #pragma unroll
-                    for (int i = 0; i < PB; ++i) pv[i] = read_block<1, false, S::P_ROWS>(ps + part_of(i) * S::P_ROWS * kSlab, block_of(i), x, lane);
+                    for (int i = 0; i < PB; ++i) pv[i] = read_block<1, false, S::P_ROWS>(p_slab(s, i), block_of(i), x, lane);
 #pragma unroll
-                    for (int h = 0; h < QB; ++h) qv[h] = read_block<1, false, S::BM>(qs, wm * QB + h, x, lane);
+                    for (int h = 0; h < QB; ++h) qv[h] = read_block<1, false, S::BM>(q_slab(s), wm * QB + h, x, lane);
 #pragma unroll
                     for (int half = 0; half < 2; ++half)
 #pragma unroll
@@ -388,18 +518,9 @@ __global__ void __launch_bounds__(WM* WN * 64) matmul_block_kernel(const FeedArg
                 for (int i = 0; i < PB; ++i)
 #pragma unroll
                     for (int h = 0; h < QB; ++h) add(i, h, c[i][h]);
+                if (s + 1 < slabs) next(s + 1);
             }
         }
-    };
-
-    load(0);
-    put(0);
-    __syncthreads();
-    for (int s = 0; s < slabs; ++s) {
-        if (s + 1 < slabs) load(s + 1);
-        compute(s);
-        if (s + 1 < slabs) put(s + 1);
-        __syncthreads();
     }
 
 #pragma unroll
@@ -416,10 +537,10 @@ __global__ void __launch_bounds__(WM* WN * 64) matmul_block_kernel(const FeedArg
     }
 }
 
-template <int DT, int FORM, int QB, int PB, int WM, int WN>
+template <int DT, int FORM, int QB, int PB, int WM, int WN, bool QD, bool PD>
 static int launch_block(FeedArgs a, void* stream) {
     using S = BlockShape<DT, FORM, QB, PB, WM, WN>;
-    auto kernel = matmul_block_kernel<DT, FORM, QB, PB, WM, WN>;
+    auto kernel = matmul_block_kernel<DT, FORM, QB, PB, WM, WN, QD, PD>;
     if constexpr (S::LDS > 64 * 1024) {
         static OncePerDevice once;
         int device = -1;
@@ -438,22 +559,43 @@ static int launch_block(FeedArgs a, void* stream) {
     return hipGetLastError() == hipSuccess ? 0 : 1;
 }
 
+// Whether an operand can go straight to LDS
+static bool direct(const FeedOperand& o, int size, bool strided) {
+    return reinterpret_cast<uintptr_t>(o.base) % 16 == 0 && o.ld % 16 == 0 && (o.padded || (strided ? o.rows : o.k) * size % 16 == 0);
+}
+static int64_t tiles(const FeedArgs& a, int64_t rows, int64_t cols) { return (a.M + rows - 1) / rows * ((a.N + cols - 1) / cols) * a.products; }
+
+template <int DT, int FORM, bool QD, bool PD>
+static int launch_shape(const FeedArgs& a, void* stream) {
+    constexpr bool LARGE = QD && PD && (DT == FEED_BF16 || DT == FEED_E4M3);
+    if constexpr (LARGE)
+        if (tiles(a, 256, FORM == FEED_GATED ? 128 : 256) >= 192) return launch_block<DT, FORM, 4, 2, 2, 4, QD, PD>(a, stream);
+    return launch_block<DT, FORM, 2, 2, 2, 2, QD, PD>(a, stream);
+}
+template <int DT, int FORM>
+static int launch_form(const FeedArgs& a, void* stream) {
+    constexpr bool Q_STRIDED = FORM == FEED_BOTH, P_STRIDED = FORM >= FEED_RIGHT;
+    const int size = feed_size(DT);
+    const bool q = direct(a.q[0], size, Q_STRIDED), p = direct(a.p[0], size, P_STRIDED) && (FORM != FEED_GATED && FORM != FEED_RIGHT || direct(a.p[1], size, P_STRIDED));
+    if constexpr (FORM >= FEED_RIGHT) return p ? launch_shape<DT, FORM, true, true>(a, stream) : launch_shape<DT, FORM, true, false>(a, stream);
+    else return q && p ? launch_shape<DT, FORM, true, true>(a, stream) : launch_shape<DT, FORM, false, false>(a, stream);
+}
 template <int DT>
-static int launch_form(const FeedArgs& a, int form, void* stream) {
+static int launch_type(const FeedArgs& a, int form, void* stream) {
     if constexpr (feed_size(DT) == 1) {
-        return form == FEED_GATED ? launch_block<DT, FEED_GATED, 2, 2, 2, 2>(a, stream) : launch_block<DT, FEED_PLAIN, 2, 2, 2, 2>(a, stream);
+        return form == FEED_GATED ? launch_form<DT, FEED_GATED>(a, stream) : launch_form<DT, FEED_PLAIN>(a, stream);
     } else {
-        if (form == FEED_GATED) return launch_block<DT, FEED_GATED, 2, 2, 2, 2>(a, stream);
-        if (form == FEED_RIGHT) return launch_block<DT, FEED_RIGHT, 2, 2, 2, 2>(a, stream);
-        return launch_block<DT, FEED_BOTH, 2, 2, 2, 2>(a, stream);
+        if (form == FEED_GATED) return launch_form<DT, FEED_GATED>(a, stream);
+        if (form == FEED_RIGHT) return launch_form<DT, FEED_RIGHT>(a, stream);
+        return launch_form<DT, FEED_BOTH>(a, stream);
     }
 }
 
 int launch_matmul(const FeedArgs& a, int form, int dtype, void* stream) {
-    if (dtype == FEED_F32) return launch_form<FEED_F32>(a, form, stream);
-    if (dtype == FEED_BF16) return launch_form<FEED_BF16>(a, form, stream);
-    if (a.out[0].size == 2) return launch_form<FEED_E4M3>(a, form, stream);
-    return launch_form<FEED_E4M3_EXACT>(a, form, stream);
+    if (dtype == FEED_F32) return launch_type<FEED_F32>(a, form, stream);
+    if (dtype == FEED_BF16) return launch_type<FEED_BF16>(a, form, stream);
+    if (a.out[0].size == 2) return launch_type<FEED_E4M3>(a, form, stream);
+    return launch_type<FEED_E4M3_EXACT>(a, form, stream);
 }
 
 }  // namespace cacnn
