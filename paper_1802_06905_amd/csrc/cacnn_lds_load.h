@@ -17,6 +17,10 @@ typedef int i32x4 __attribute__((ext_vector_type(4)));
 __device__ __forceinline__ void load_to_lds_unseen(i32x4 d, uint32_t off, uint32_t dst) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(dst), "v"(off), "s"(d) : "memory", "m0");
 }
+// 64 lanes x 4 bytes, lane L's to LDS byte dst + 4 L
+__device__ __forceinline__ void load_word_to_lds_unseen(i32x4 d, uint32_t off, uint32_t dst) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"(dst), "v"(off), "s"(d) : "memory", "m0");
+}
 #pragma clang diagnostic pop
 
 }  // namespace cacnn

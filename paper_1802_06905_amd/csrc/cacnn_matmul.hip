@@ -183,6 +183,7 @@ struct DirectLoader {
         for (int i = 0; i < Map::N; ++i) load_to_lds_unseen(d, off[i] + more, slab + (i * WAVES + wave) * 1024);
     }
 };
+__device__ __forceinline__ uint32_t lds_address(const char* p) { return (uint32_t)(uintptr_t)(MAT_LDS(const char)*)p; }
 __device__ __forceinline__ void loads_done() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 __device__ __forceinline__ void lds_done() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
 
@@ -194,7 +195,7 @@ struct Loader {
     __device__ __forceinline__ void init(const FeedOperand& o, int64_t row0, int wave, int lane) { l.init(o, row0, wave, lane); }
     __device__ __forceinline__ void move(const FeedOperand& o, int64_t row0) { l.move(o, row0); }
     // begins to bring slab s, to `slab`: now, or with put() after the loads have come
-    __device__ __forceinline__ void begin(int s, bool any, char* slab) { l.issue(s, any, (uint32_t)(uintptr_t)(MAT_LDS(char)*)slab); }
+    __device__ __forceinline__ void begin(int s, bool any, char* slab) { l.issue(s, any, lds_address(slab)); }
     __device__ __forceinline__ void put(char*) {}
 };
 template <int ESZ, bool STRIDED, int ROWS, int WAVES>
@@ -367,7 +368,10 @@ __global__ void __launch_bounds__(WM* WN * 64, WM* WN == 4 ? 2 : 1) matmul_block
 #pragma unroll
     for (int h = 0; h < S::P_PARTS; ++h) p[h].init(a.p[h], n0, wave, lane);
     const int per_segment = (int)((a.q[0].k + KE - 1) / KE), slabs = max(1, per_segment * a.segments);
-    float row_scale = 0.f;
+    // 8 bits: the scales of a slab's rows, a word each, brought by as many waves as they fill (rows behind the last: zeros)
+    const bool brings_scales = ESZ == 1 && wave * 64 < S::BM;
+    const i32x4 scales = ESZ == 1 ? bytes_from((const char*)(a.q_scale + m0 * a.scale_cols), min((int64_t)S::BM, a.M - m0) * a.scale_cols * 4) : i32x4{0, 0, 0, 0};
+    const uint32_t scale_off = (uint32_t)threadIdx.x * a.scale_cols * 4;
     // Slab s on its way to its half of LDS, and there
     auto begin = [&](int s) {
         char* const stage = s_mem + (s & 1) * S::STAGE;
@@ -383,15 +387,13 @@ __global__ void __launch_bounds__(WM* WN * 64, WM* WN == 4 ? 2 : 1) matmul_block
 #pragma unroll
         for (int h = 0; h < S::P_PARTS; ++h) p[h].begin(i, any, stage + S::Q_BYTES + h * S::P_ROWS * kSlab);
         if constexpr (ESZ == 1)
-            if ((int)threadIdx.x < S::BM && any && m0 + threadIdx.x < a.M) row_scale = a.q_scale[(m0 + threadIdx.x) * a.scale_cols + i];
+            if (brings_scales) load_word_to_lds_unseen(scales, scale_off + i * 4, lds_address(stage + S::Q_BYTES + S::P_BYTES + wave * 256));
     };
     auto put = [&](int s) {
         char* const stage = s_mem + (s & 1) * S::STAGE;
         q.put(stage);
 #pragma unroll
         for (int h = 0; h < S::P_PARTS; ++h) p[h].put(stage + S::Q_BYTES + h * S::P_ROWS * kSlab);
-        if constexpr (ESZ == 1)
-            if ((int)threadIdx.x < S::BM) *(float*)(stage + S::Q_BYTES + S::P_BYTES + threadIdx.x * 4) = row_scale;
     };
     // a wave's i-th block of columns: part of p, block within it
     auto part_of = [&](int i) { return S::GATED ? i / (PB / 2) : 0; };
@@ -464,20 +466,30 @@ __global__ void __launch_bounds__(WM* WN * 64, WM* WN == 4 ? 2 : 1) matmul_block
                 const float f = sp[i] * sq[h];
 #pragma unroll
                 for (int v = 0; v < 16; ++v) acc[i][h][v] = __builtin_fmaf(c[v], f, acc[i][h][v]);
+                // (here and now: the compiler puts all of them off to the end of the slab, with a register for every product until then)
+                asm volatile("" : "+v"(acc[i][h]));
             };
             if constexpr (DT == FEED_E4M3) {
+                // (one address for each of the four chunks and operand, the blocks at constant distances: more and the sums spill)
+                const uint32_t qa = lds_address(q_slab(s)) + (wm * QB * 32 + j) * kSlab, pa = lds_address(q_slab(s)) + S::Q_BYTES + (block_of(0) * 32 + j) * kSlab;
+                uint32_t chunk[4];
+#pragma unroll
+                for (int x = 0; x < 4; ++x) chunk[x] = ((2 * x + g) ^ (j & 7)) * 16;
+                auto chunk_at = [](uint32_t at, int more) { return *(MAT_LDS(const mu32x4)*)((MAT_LDS(const char)*)(uintptr_t)at + more); };
                 mu32x4 pv[PB][2][2], qv[2][2];
                 auto read_q = [&](int h) {
 #pragma unroll
-                    for (int x = 0; x < 4; ++x) qv[x / 2][x % 2] = read_block<1, false, S::BM>(q_slab(s), wm * QB + h, x, lane);
+                    for (int x = 0; x < 4; ++x) qv[x / 2][x % 2] = chunk_at(qa + chunk[x], h * 32 * kSlab);
                 };
 #pragma unroll
                 for (int i = 0; i < PB; ++i)
 #pragma unroll
-                    for (int x = 0; x < 4; ++x) pv[i][x / 2][x % 2] = read_block<1, false, S::P_ROWS>(p_slab(s, i), block_of(i), x, lane);
+                    for (int x = 0; x < 4; ++x)
+                        pv[i][x / 2][x % 2] = chunk_at(pa + chunk[x], (part_of(i) * S::P_ROWS + (block_of(i) - block_of(0)) * 32) * kSlab);
                 read_q(0);
 #pragma unroll
                 for (int h = 0; h < QB; ++h) {
+                    if (h + 1 == QB && s + 1 < slabs) next(s + 1);
                     mf32x16 c[PB];
 #pragma unroll
                     for (int i = 0; i < PB; ++i) {
@@ -487,10 +499,9 @@ __global__ void __launch_bounds__(WM* WN * 64, WM* WN == 4 ? 2 : 1) matmul_block
                     }
                     __builtin_amdgcn_sched_barrier(0);
                     if (h + 1 < QB) read_q(h + 1);
-                    else if (s + 1 < slabs) next(s + 1);
-                    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
                     for (int i = 0; i < PB; ++i) add(i, h, c[i]);
+                    __builtin_amdgcn_sched_barrier(0);
                 }
             } else {
                 mf32x16 c[PB][QB];
