@@ -15,6 +15,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <cmath>
+
 #include "cacnn_feed.h"
 #include "cacnn_gate.h"
 #include "cacnn_internal.h"
@@ -28,6 +30,8 @@ typedef int mi32x8 __attribute__((ext_vector_type(8)));
 typedef unsigned int mu32x2 __attribute__((ext_vector_type(2)));
 typedef unsigned int mu32x4 __attribute__((ext_vector_type(4)));
 typedef short ms16x4 __attribute__((ext_vector_type(4)));
+// (a lambda that is called twice may stay a function, with everything it refers to in memory)
+#define MAT_INLINE __attribute__((always_inline))
 typedef __bf16 mbf16x8 __attribute__((ext_vector_type(8)));
 #define MAT_LDS(T) __attribute__((address_space(3))) T
 #define MAT_CONST(T) __attribute__((address_space(4))) const T
@@ -35,8 +39,6 @@ typedef __bf16 mbf16x8 __attribute__((ext_vector_type(8)));
 struct __attribute__((packed, aligned(1))) MatBytes16 {
     mu32x4 v;
 };
-
-constexpr int kSlab = 128;   // bytes of a row and slab
 
 // Where the strided operand's block b of contraction index k lies: b ^ strided_turn.  The lanes of one access have k = 8 g + (0..3) (bf16, blocks of
 // 64 bytes) or 4 g + e (fp32, blocks of 128), g = 0 and 1.
@@ -49,13 +51,16 @@ __device__ __forceinline__ int strided_turn(int k) {
 
 // What a lane's i-th 16 bytes of a slab are: the slab's 16-byte pieces in the order in which they lie in LDS, dealt to the lanes
 // of a wave, 1024 bytes at a time, in turns to the waves.
-template <int ESZ, bool STRIDED, int ROWS, int WAVES>
+// SLAB: bytes of a row and slab, 64 or 128.
+__device__ __forceinline__ int chunk_turn(int slab, int row) { return slab == 128 ? (row >> 1) & 7 : (row >> 2) & 3; }
+template <int ESZ, bool STRIDED, int ROWS, int WAVES, int SLAB>
 struct SlabMap {
-    static constexpr int N = ROWS * kSlab / 1024 / WAVES, KR = kSlab / ESZ, LANES = ROWS * ESZ / 16;   // pieces a lane; indices a slab; lanes a strided row
-    static_assert(N >= 1 && N * WAVES * 1024 == ROWS * kSlab, "a slab is whole wave loads");
+    static constexpr int N = ROWS * SLAB / 1024 / WAVES, KR = SLAB / ESZ, LANES = ROWS * ESZ / 16;   // pieces a lane; indices a slab; lanes a strided row
+    static constexpr int CHUNKS = SLAB / 16;
+    static_assert(N >= 1 && N * WAVES * 1024 == ROWS * SLAB, "a slab is whole wave loads");
     // contiguous: row and byte of the slab's row
-    static __device__ __forceinline__ int row(int i, int wave, int lane) { return (i * WAVES + wave) * 8 + (lane >> 3); }
-    static __device__ __forceinline__ int byte(int lane) { return ((lane & 7) ^ (lane >> 3)) * 16; }
+    static __device__ __forceinline__ int row(int i, int wave, int lane) { return (i * WAVES + wave) * (64 / CHUNKS) + lane / CHUNKS; }
+    static __device__ __forceinline__ int byte(int i, int wave, int lane) { return (lane % CHUNKS ^ chunk_turn(SLAB, row(i, wave, lane))) * 16; }
     // strided: contraction index within the slab, and byte of that row
     static __device__ __forceinline__ int index(int i, int wave, int lane) { return (i * WAVES + wave) * (64 / LANES) + lane / LANES; }
     static __device__ __forceinline__ int column(int i, int wave, int lane) {
@@ -65,56 +70,99 @@ struct SlabMap {
     }
 };
 
-// Brings slabs to LDS through registers, from any address and of any size: whole 16 bytes where the array has them, else element by element
-// with zeros behind its end.
-template <int ESZ, bool STRIDED, int ROWS, int WAVES>
+// 16 bytes moved down by `bytes` (0 to 16), zeros behind them
+__device__ __forceinline__ mu32x4 moved_down(mu32x4 v, int bytes) {
+    if (bytes & 4) v = mu32x4{v[1], v[2], v[3], 0};
+    if (bytes & 8) v = mu32x4{v[2], v[3], 0, 0};
+    if (bytes & 16) v = mu32x4{0, 0, 0, 0};
+    const int b = bytes & 3;
+    return mu32x4{__builtin_amdgcn_alignbyte(v[1], v[0], b), __builtin_amdgcn_alignbyte(v[2], v[1], b), __builtin_amdgcn_alignbyte(v[3], v[2], b),
+                  __builtin_amdgcn_alignbyte(0, v[3], b)};
+}
+
+// Brings slabs to LDS through registers, from any address and of any size, 16 bytes a load.  A piece that the end of a row cuts is loaded as the row's
+// last 16 bytes and moved down when it has come; what lies behind the last contraction index becomes zeros, rows and columns behind the last stand for
+// it again (what comes of them is not stored).  Rows of less than 16 bytes are read element by element.
+// (With the cut pieces read element by element the tiles at the edge took as long as all others together: bf16 (2048, 2047, 4095), the gradient
+// of x, 577 us then and 198 now.)
+template <int ESZ, bool STRIDED, int ROWS, int WAVES, int SLAB>
 struct RegisterLoader {
-    using Map = SlabMap<ESZ, STRIDED, ROWS, WAVES>;
+    using Map = SlabMap<ESZ, STRIDED, ROWS, WAVES, SLAB>;
     const char* base;
-    int64_t ld, k, k0;
+    int64_t ld, k;
     int rows, wave, lane;
+    bool tiny, cut;                // rows of less than 16 bytes; the last slab's pieces have to be moved
+    int off[Map::N];               // (in a tile of few columns the row's last 16 bytes begin before it)
+    int down[Map::N], edge[Map::N];    // bytes to move the slab's pieces by, and (strided) those at the last column
     mu32x4 r[Map::N];
 
     __device__ __forceinline__ void init(const FeedOperand& o, int64_t row0, int wave_, int lane_) {
         ld = o.ld, k = o.k, wave = wave_, lane = lane_;
-        base = o.base + (STRIDED ? row0 * ESZ : row0 * ld);
         rows = (int)max((int64_t)0, min((int64_t)ROWS, o.rows - row0));
-    }
-    // slab s of the operand (none if !any: zeros)
-    __device__ __forceinline__ void load(int64_t s, bool any) {
+        tiny = (STRIDED ? o.rows : k) * ESZ < 16;
+        move(o, row0);
 #pragma unroll
         for (int i = 0; i < Map::N; ++i) {
-            const char* p;
-            int64_t left;                                                         // bytes from p on that belong to the operand
+            edge[i] = 0;
             if constexpr (STRIDED) {
-                const int64_t at = s * Map::KR + Map::index(i, wave, lane);
-                const int col = Map::column(i, wave, lane);
-                p = base + at * ld + col;
-                left = any && at < k ? (int64_t)rows * ESZ - col : 0;
+                const int col = Map::column(i, wave, lane), left = rows * ESZ - col;
+                edge[i] = left >= 16 || tiny ? 0 : left > 0 ? 16 - left : 16;
+                off[i] = Map::index(i, wave, lane) * (int)ld + (left >= 16 || tiny ? col : rows * ESZ - 16);
             } else {
-                const int row = Map::row(i, wave, lane);
-                const int64_t at = s * kSlab + Map::byte(lane);
-                p = base + row * ld + at;
-                left = any && row < rows ? k * ESZ - at : 0;
+                off[i] = min(Map::row(i, wave, lane), max(rows - 1, 0)) * (int)ld + Map::byte(i, wave, lane);
             }
-            mu32x4 v = {0, 0, 0, 0};
-            if (left >= 16) {
-                v = ((const MatBytes16*)p)->v;
-            } else if (left > 0) {
+        }
+    }
+    __device__ __forceinline__ void move(const FeedOperand& o, int64_t row0) { base = o.base + (STRIDED ? row0 * ESZ : row0 * ld); }
+    // slab s of the operand (none if !any: zeros)
+    __device__ __forceinline__ void load(int64_t s, bool any) {
+        const char* const from = base + (STRIDED ? s * Map::KR * ld : s * SLAB);
+        any = any && rows > 0;
+        cut = STRIDED && rows < ROWS;
+        if (any && !tiny && (STRIDED ? (s + 1) * Map::KR <= k : (s + 1) * SLAB <= k * ESZ)) {
+#pragma unroll
+            for (int i = 0; i < Map::N; ++i) {
+                down[i] = edge[i];
+                r[i] = ((const MatBytes16*)(from + off[i]))->v;
+            }
+            return;
+        }
+        cut = true;
+#pragma unroll
+        for (int i = 0; i < Map::N; ++i) {
+            r[i] = mu32x4{0, 0, 0, 0};
+            down[i] = 0;
+            if (!any) continue;
+            if (tiny) {
+                // elements of this piece that belong to the operand
+                int64_t left;
+                if constexpr (STRIDED) left = s * Map::KR + Map::index(i, wave, lane) < k ? rows * ESZ - Map::column(i, wave, lane) : 0;
+                else left = Map::row(i, wave, lane) < rows ? k * ESZ - s * SLAB - Map::byte(i, wave, lane) : 0;
 #pragma unroll
                 for (int e = 0; e < 16 / ESZ; ++e)
                     if (e * ESZ < left) {
+                        const char* const p = from + off[i];
                         uint32_t x;
                         if constexpr (ESZ == 4) x = *(const uint32_t*)(p + e * 4);
                         else if constexpr (ESZ == 2) x = *(const uint16_t*)(p + e * 2);
                         else x = *(const uint8_t*)(p + e);
-                        v[e * ESZ / 4] |= x << (e * ESZ % 4 * 8);
+                        r[i][e * ESZ / 4] |= x << (e * ESZ % 4 * 8);
                     }
+            } else if constexpr (STRIDED) {
+                const bool there = s * Map::KR + Map::index(i, wave, lane) < k;
+                down[i] = there ? edge[i] : 16;
+                if (there) r[i] = ((const MatBytes16*)(from + off[i]))->v;
+            } else {
+                const int left = (int)(k * ESZ - s * SLAB) - Map::byte(i, wave, lane);
+                down[i] = left >= 16 ? 0 : left > 0 ? 16 - left : 16;
+                if (left > 0) r[i] = ((const MatBytes16*)(from + off[i] - down[i]))->v;
             }
-            r[i] = v;
         }
     }
     __device__ __forceinline__ void put(char* slab) {
+        if (cut)
+#pragma unroll
+            for (int i = 0; i < Map::N; ++i) r[i] = moved_down(r[i], down[i]);
 #pragma unroll
         for (int i = 0; i < Map::N; ++i) *(mu32x4*)(slab + (i * WAVES + wave) * 1024 + lane * 16) = r[i];
     }
@@ -132,18 +180,18 @@ __device__ __forceinline__ i32x4 bytes_from(const char* p, int64_t bytes) {
     d[3] = 0x00020000;
     return d;
 }
-template <int ESZ, bool STRIDED, int ROWS, int WAVES>
+template <int ESZ, bool STRIDED, int ROWS, int WAVES, int SLAB>
 struct DirectLoader {
-    using Map = SlabMap<ESZ, STRIDED, ROWS, WAVES>;
+    using Map = SlabMap<ESZ, STRIDED, ROWS, WAVES, SLAB>;
     const char* base;
     int64_t ld, k;
     int bytes;                     // contiguous: of a row; strided: of a row of the tile; whole pieces of 16
-    int byte, wave;
+    int wave, lane;
     i32x4 d;
-    uint32_t off[Map::N];
+    uint32_t off[Map::N], at;
 
-    __device__ __forceinline__ void init(const FeedOperand& o, int64_t row0, int wave_, int lane) {
-        wave = wave_, ld = o.ld, k = o.k;
+    __device__ __forceinline__ void init(const FeedOperand& o, int64_t row0, int wave_, int lane_) {
+        wave = wave_, lane = lane_, ld = o.ld, k = o.k;
         const int rows = (int)max((int64_t)0, min((int64_t)ROWS, o.rows - row0));
         base = o.base + (STRIDED ? row0 * ESZ : row0 * ld);
         if constexpr (STRIDED) {
@@ -155,12 +203,11 @@ struct DirectLoader {
             }
         } else {
             bytes = (int)((k * ESZ + 15) & ~15);
-            byte = Map::byte(lane);
             d = bytes_from(base, rows ? (int64_t)(rows - 1) * ld + bytes : 0);
 #pragma unroll
             for (int i = 0; i < Map::N; ++i) {
                 const int row = Map::row(i, wave, lane);
-                off[i] = row < rows ? (uint32_t)row * (uint32_t)ld + byte : kOutside;
+                off[i] = row < rows ? (uint32_t)row * (uint32_t)ld + Map::byte(i, wave, lane) : kOutside;
             }
         }
     }
@@ -169,18 +216,20 @@ struct DirectLoader {
         base = o.base + (STRIDED ? row0 * ESZ : row0 * ld);
         if constexpr (!STRIDED) d = bytes_from(base, (uint32_t)d[2]);
     }
-    // slab s (none if !any: zeros) to LDS bytes `slab`
-    __device__ __forceinline__ void issue(int s, bool any, uint32_t slab) {
-        uint32_t more = 0;
+    // Slab s (none if !any: zeros) is the one that issue() brings, a load at a time
+    __device__ __forceinline__ void prepare(int s, bool any) {
         if constexpr (STRIDED) {
-            const int64_t at = (int64_t)s * Map::KR;
-            const int64_t left = any ? min(k - at, (int64_t)Map::KR) : 0;
-            d = bytes_from(base + at * ld, left > 0 ? (left - 1) * ld + bytes : 0);
+            const int64_t from = (int64_t)s * Map::KR;
+            const int64_t left = any ? min(k - from, (int64_t)Map::KR) : 0;
+            d = bytes_from(base + from * ld, left > 0 ? (left - 1) * ld + bytes : 0);
         } else {
-            more = any && s * kSlab + byte < bytes ? s * kSlab : kOutside;
+            at = any ? (uint32_t)(s * SLAB) : kOutside;
         }
-#pragma unroll
-        for (int i = 0; i < Map::N; ++i) load_to_lds_unseen(d, off[i] + more, slab + (i * WAVES + wave) * 1024);
+    }
+    __device__ __forceinline__ void issue(int i, uint32_t slab) {
+        uint32_t more = 0;
+        if constexpr (!STRIDED) more = at + Map::byte(i, wave, lane) < (uint32_t)bytes ? at : kOutside;
+        load_to_lds_unseen(d, off[i] + more, slab + (i * WAVES + wave) * 1024);
     }
 };
 __device__ __forceinline__ uint32_t lds_address(const char* p) { return (uint32_t)(uintptr_t)(MAT_LDS(const char)*)p; }
@@ -188,32 +237,34 @@ __device__ __forceinline__ void loads_done() { asm volatile("s_waitcnt vmcnt(0)"
 __device__ __forceinline__ void lds_done() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
 
 // One operand's way to LDS
-template <int ESZ, bool STRIDED, int ROWS, int WAVES, bool DIRECT>
+template <int ESZ, bool STRIDED, int ROWS, int WAVES, int SLAB, bool DIRECT>
 struct Loader {
-    static constexpr bool direct = DIRECT;
-    DirectLoader<ESZ, STRIDED, ROWS, WAVES> l;
+    static constexpr int LOADS = SlabMap<ESZ, STRIDED, ROWS, WAVES, SLAB>::N;
+    DirectLoader<ESZ, STRIDED, ROWS, WAVES, SLAB> l;
     __device__ __forceinline__ void init(const FeedOperand& o, int64_t row0, int wave, int lane) { l.init(o, row0, wave, lane); }
     __device__ __forceinline__ void move(const FeedOperand& o, int64_t row0) { l.move(o, row0); }
-    // begins to bring slab s, to `slab`: now, or with put() after the loads have come
-    __device__ __forceinline__ void begin(int s, bool any, char* slab) { l.issue(s, any, lds_address(slab)); }
+    // slab s is brought by the LOADS calls of issue() that follow, or by put() after the loads that prepare() made have come
+    __device__ __forceinline__ void prepare(int s, bool any) { l.prepare(s, any); }
+    __device__ __forceinline__ void issue(int i, uint32_t slab) { l.issue(i, slab); }
     __device__ __forceinline__ void put(char*) {}
 };
-template <int ESZ, bool STRIDED, int ROWS, int WAVES>
-struct Loader<ESZ, STRIDED, ROWS, WAVES, false> {
-    static constexpr bool direct = false;
-    RegisterLoader<ESZ, STRIDED, ROWS, WAVES> l;
+template <int ESZ, bool STRIDED, int ROWS, int WAVES, int SLAB>
+struct Loader<ESZ, STRIDED, ROWS, WAVES, SLAB, false> {
+    static constexpr int LOADS = 0;
+    RegisterLoader<ESZ, STRIDED, ROWS, WAVES, SLAB> l;
     __device__ __forceinline__ void init(const FeedOperand& o, int64_t row0, int wave, int lane) { l.init(o, row0, wave, lane); }
-    __device__ __forceinline__ void move(const FeedOperand& o, int64_t row0) { l.base = o.base + (STRIDED ? row0 * ESZ : row0 * l.ld); }
-    __device__ __forceinline__ void begin(int s, bool any, char*) { l.load(s, any); }
+    __device__ __forceinline__ void move(const FeedOperand& o, int64_t row0) { l.move(o, row0); }
+    __device__ __forceinline__ void prepare(int s, bool any) { l.load(s, any); }
+    __device__ __forceinline__ void issue(int, uint32_t) {}
     __device__ __forceinline__ void put(char* slab) { l.put(slab); }
 };
 
 // A block of 32 rows (or columns) of step `st` of a slab, as the matrix instructions take it: 16 bytes a lane
-template <int ESZ, bool STRIDED, int ROWS>
+template <int ESZ, bool STRIDED, int ROWS, int SLAB>
 __device__ __forceinline__ mu32x4 read_block(const char* slab, int block, int st, int lane) {
     const int j = lane & 31, g = lane >> 5;
     if constexpr (!STRIDED) {
-        return *(const mu32x4*)(slab + (block * 32 + j) * kSlab + (((2 * st + g) ^ (j & 7)) * 16));
+        return *(const mu32x4*)(slab + (block * 32 + j) * SLAB + (((2 * st + g) ^ chunk_turn(SLAB, j)) * 16));
     } else if constexpr (ESZ == 4) {
         mu32x4 v;
         const int k = 8 * st + 4 * g;
@@ -341,73 +392,107 @@ __device__ __forceinline__ TilePlace tile_place(const FeedArgs& a, int wg) {
 }
 
 // QB x PB blocks of 32 x 32 to a wave, WM x WN waves.  GATED: half of a wave's columns are of the gate, the others the same ones of up.
-template <int DT, int FORM, int QB, int PB, int WM, int WN>
+// Of STAGES slabs one is multiplied, the others are in LDS or on their way.
+template <int DT, int FORM, int QB, int PB, int WM, int WN, int SLAB, int STAGES>
 struct BlockShape {
     static constexpr int ESZ = feed_size(DT), WAVES = WM * WN, BM = WM * QB * 32, BN = WN * PB * 32;
     static constexpr bool GATED = FORM == FEED_GATED, Q_STRIDED = FORM == FEED_BOTH, P_STRIDED = FORM >= FEED_RIGHT;
     static constexpr int COLS = GATED ? BN / 2 : BN;                    // of Out
     static constexpr int P_PARTS = GATED ? 2 : 1, P_ROWS = BN / P_PARTS;
-    static constexpr int Q_BYTES = BM * kSlab, P_BYTES = BN * kSlab, SCALES = ESZ == 1 ? BM * 4 : 0;
-    static constexpr int STAGE = Q_BYTES + P_BYTES + SCALES, LDS = 2 * STAGE;
+    static constexpr int Q_BYTES = BM * SLAB, P_BYTES = BN * SLAB, SCALES = ESZ == 1 ? BM * 4 : 0;
+    static constexpr int STAGE = Q_BYTES + P_BYTES + SCALES, LDS = STAGES * STAGE;
+    static_assert(ESZ > 1 || SLAB == kScaleBlock, "a slab in 8 bits has one scale");
 };
 
 // QD, PD: whether the operands go straight to LDS.
-template <int DT, int FORM, int QB, int PB, int WM, int WN, bool QD, bool PD>
+template <int DT, int FORM, int QB, int PB, int WM, int WN, int SLAB, int STAGES, bool QD, bool PD>
 __global__ void __launch_bounds__(WM* WN * 64, WM* WN == 4 ? 2 : 1) matmul_block_kernel(const FeedArgs a) {
-    using S = BlockShape<DT, FORM, QB, PB, WM, WN>;
-    constexpr int ESZ = S::ESZ, WAVES = S::WAVES, KE = kSlab / ESZ;
+    using S = BlockShape<DT, FORM, QB, PB, WM, WN, SLAB, STAGES>;
+    constexpr int ESZ = S::ESZ, WAVES = S::WAVES, KE = SLAB / ESZ;
+    static_assert(STAGES == 2 || (QD && PD), "operands that come through registers are one slab ahead");
     extern __shared__ __align__(16) char s_mem[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave % WM, wn = wave / WM, j = lane & 31, g = lane >> 5;
     const TilePlace at = tile_place(a, blockIdx.x);
     const int64_t m0 = (int64_t)at.m * S::BM, n0 = (int64_t)at.n * S::COLS;
 
-    Loader<ESZ, S::Q_STRIDED, S::BM, WAVES, QD> q;
-    Loader<ESZ, S::P_STRIDED, S::P_ROWS, WAVES, PD> p[S::P_PARTS];
+    using QLoader = Loader<ESZ, S::Q_STRIDED, S::BM, WAVES, SLAB, QD>;
+    using PLoader = Loader<ESZ, S::P_STRIDED, S::P_ROWS, WAVES, SLAB, PD>;
+    constexpr int LOADS = QLoader::LOADS + S::P_PARTS * PLoader::LOADS + (ESZ == 1 ? 1 : 0);    // of a wave and slab
+    QLoader q;
+    PLoader p0, p1;                                            // (p1: of up, where there is one)
     q.init(a.q[at.product], m0, wave, lane);
-#pragma unroll
-    for (int h = 0; h < S::P_PARTS; ++h) p[h].init(a.p[h], n0, wave, lane);
+    p0.init(a.p[0], n0, wave, lane);
+    if constexpr (S::GATED) p1.init(a.p[1], n0, wave, lane);
     const int per_segment = (int)((a.q[0].k + KE - 1) / KE), slabs = max(1, per_segment * a.segments);
-    // 8 bits: the scales of a slab's rows, a word each, brought by as many waves as they fill (rows behind the last: zeros)
-    const bool brings_scales = ESZ == 1 && wave * 64 < S::BM;
+    // 8 bits: the scales of a slab's rows, a word each, 64 rows a wave (rows behind the last: zeros; more waves bring the same again, so that
+    // every wave has as many loads on their way)
+    const int scale_wave = wave % (S::BM / 64);
     const i32x4 scales = ESZ == 1 ? bytes_from((const char*)(a.q_scale + m0 * a.scale_cols), min((int64_t)S::BM, a.M - m0) * a.scale_cols * 4) : i32x4{0, 0, 0, 0};
-    const uint32_t scale_off = (uint32_t)threadIdx.x * a.scale_cols * 4;
-    // Slab s on its way to its half of LDS, and there
-    auto begin = [&](int s) {
-        char* const stage = s_mem + (s & 1) * S::STAGE;
-        int i = s;
+    const uint32_t scale_off = (uint32_t)(scale_wave * 64 + lane) * a.scale_cols * 4;
+    // Slab s is the one that load_some() brings (behind the last: zeros, so that the loads on their way can be counted)
+    const uint32_t lds = lds_address(s_mem);
+    uint32_t coming = lds;
+    int coming_slab = 0;
+    auto prepare = [&](int s, int at_stage) MAT_INLINE {
+        coming = lds + at_stage * S::STAGE;
+        coming_slab = s;
         if constexpr (FORM == FEED_RIGHT)
             if (s >= per_segment && a.segments > 1) {
-                i = s - per_segment;
+                coming_slab = s - per_segment;
                 q.move(a.q[1], m0);
-                p[0].move(a.p[1], n0);
+                p0.move(a.p[1], n0);
             }
-        const bool any = i < per_segment;
-        q.begin(i, any, stage);
-#pragma unroll
-        for (int h = 0; h < S::P_PARTS; ++h) p[h].begin(i, any, stage + S::Q_BYTES + h * S::P_ROWS * kSlab);
-        if constexpr (ESZ == 1)
-            if (brings_scales) load_word_to_lds_unseen(scales, scale_off + i * 4, lds_address(stage + S::Q_BYTES + S::P_BYTES + wave * 256));
+        const bool any = s < slabs && coming_slab < per_segment;
+        q.prepare(coming_slab, any);
+        p0.prepare(coming_slab, any);
+        if constexpr (S::GATED) p1.prepare(coming_slab, any);
     };
-    auto put = [&](int s) {
-        char* const stage = s_mem + (s & 1) * S::STAGE;
-        q.put(stage);
+    auto load_some = [&](int from, int to) MAT_INLINE {
 #pragma unroll
-        for (int h = 0; h < S::P_PARTS; ++h) p[h].put(stage + S::Q_BYTES + h * S::P_ROWS * kSlab);
+        for (int l = from; l < to; ++l) {
+            if constexpr (QD)
+                if (l < QLoader::LOADS) q.issue(l, coming);
+            if constexpr (PD) {
+                const int i = l - QLoader::LOADS;
+                if (i >= 0 && i < PLoader::LOADS) p0.issue(i, coming + S::Q_BYTES);
+                if constexpr (S::GATED)
+                    if (i >= PLoader::LOADS && i < 2 * PLoader::LOADS) p1.issue(i - PLoader::LOADS, coming + S::Q_BYTES + S::P_ROWS * SLAB);
+            }
+            if constexpr (ESZ == 1)
+                if (l == LOADS - 1)
+                    load_word_to_lds_unseen(scales, scale_off + coming_slab * 4, coming + S::Q_BYTES + S::P_BYTES + scale_wave * 256);
+        }
+    };
+    auto put = [&](int at_stage) MAT_INLINE {
+        char* const stage = s_mem + at_stage * S::STAGE;
+        q.put(stage);
+        p0.put(stage + S::Q_BYTES);
+        if constexpr (S::GATED) p1.put(stage + S::Q_BYTES + S::P_ROWS * SLAB);
     };
     // a wave's i-th block of columns: part of p, block within it
     auto part_of = [&](int i) { return S::GATED ? i / (PB / 2) : 0; };
     auto block_of = [&](int i) { return S::GATED ? wn * (PB / 2) + i % (PB / 2) : wn * PB + i; };
-    auto q_slab = [&](int s) -> const char* { return s_mem + (s & 1) * S::STAGE; };
-    auto p_slab = [&](int s, int i) -> const char* { return s_mem + (s & 1) * S::STAGE + S::Q_BYTES + part_of(i) * S::P_ROWS * kSlab; };
-    // This wave has read what it needs of slab s - 1, and slab s is there for all; the buffer of slab s - 1 takes slab s + 1
-    auto next = [&](int s) {
-        loads_done();
-        put(s);
+    int stage = 0;                                             // of the slab that is multiplied
+    auto q_slab = [&](int at_stage) -> const char* { return s_mem + at_stage * S::STAGE; };
+    auto p_slab = [&](int at_stage, int i) -> const char* { return s_mem + at_stage * S::STAGE + S::Q_BYTES + part_of(i) * S::P_ROWS * SLAB; };
+    // This wave has read what it needs of slab s - 1, and slab s is there for all; the stage of slab s - 1 takes the next one
+    auto next = [&](int s) MAT_INLINE {
+        const int free = stage;
+        stage = stage + 1 == STAGES ? 0 : stage + 1;
+        asm volatile("s_waitcnt vmcnt(%0)" ::"n"((STAGES - 2) * LOADS) : "memory");
+        put(stage);
         lds_done();
         __builtin_amdgcn_s_barrier();
-        if (s + 1 < slabs) begin(s + 1);
+        prepare(s + STAGES - 1, free);
         asm volatile("" ::: "memory");
+    };
+    // Between two calls of next() the wave multiplies several times, and behind each brings a part of the next slab: all at once, the loads keep it
+    // from issuing products for as long as those of all waves take to be accepted (bf16, 256 x 256: 1012 -> 977 us for 1.1 PFLOP).  With two stages there is one slab only between a load
+    // and its wait: early, in one go with four waves, in two with eight (128 x 128 tiles 3 to 20 % slower if spread).
+    auto phase_of = [](int phase, int phases) {
+        const int n = STAGES > 2 ? phases : WAVES > 4 ? 2 : 1;
+        return min(LOADS, (LOADS + n - 1) / n * phase);
     };
 
     mf32x16 acc[PB][QB];
@@ -418,38 +503,50 @@ __global__ void __launch_bounds__(WM* WN * 64, WM* WN == 4 ? 2 : 1) matmul_block
 #pragma unroll
             for (int v = 0; v < 16; ++v) acc[i][h][v] = 0.f;
 
-    begin(0);
+#pragma unroll
+    for (int s = 0; s < STAGES - 1; ++s) {
+        prepare(s, s);
+        load_some(0, LOADS);
+    }
+    stage = STAGES - 1;
     next(0);
+    if constexpr (DT == FEED_E4M3) load_some(0, phase_of(1, QB));
+    if constexpr (DT == FEED_E4M3_EXACT) load_some(0, LOADS);
     if constexpr (ESZ > 1) {
         // The operands of a step are read under the products of the step before, across slabs too
         mu32x4 pv[2][PB], qv[2][QB];
-        auto read = [&](int s, int st, int set) {
+        auto read = [&](int st, int set) MAT_INLINE {
 #pragma unroll
-            for (int i = 0; i < PB; ++i) pv[set][i] = read_block<ESZ, S::P_STRIDED, S::P_ROWS>(p_slab(s, i), block_of(i), st, lane);
+            for (int i = 0; i < PB; ++i) pv[set][i] = read_block<ESZ, S::P_STRIDED, S::P_ROWS, SLAB>(p_slab(stage, i), block_of(i), st, lane);
 #pragma unroll
-            for (int h = 0; h < QB; ++h) qv[set][h] = read_block<ESZ, S::Q_STRIDED, S::BM>(q_slab(s), wm * QB + h, st, lane);
+            for (int h = 0; h < QB; ++h) qv[set][h] = read_block<ESZ, S::Q_STRIDED, S::BM, SLAB>(q_slab(stage), wm * QB + h, st, lane);
             __builtin_amdgcn_sched_barrier(0);
         };
-        auto products = [&](int set) {
+        constexpr int STEPS = SLAB / 32;
+        auto products = [&](int set, int phase) MAT_INLINE {
 #pragma unroll
-            for (int i = 0; i < PB; ++i)
+            for (int i = 0; i < PB; ++i) {
 #pragma unroll
                 for (int h = 0; h < QB; ++h) multiply<DT>(acc[i][h], pv[set][i], qv[set][h]);
-            __builtin_amdgcn_sched_barrier(0);
-        };
-        read(0, 0, 0);
-        for (int s = 0; s < slabs; ++s) {
-            read(s, 1, 1);
-            products(0);
-            read(s, 2, 0);
-            products(1);
-            read(s, 3, 1);
-            products(0);
-            if (s + 1 < slabs) {
-                next(s + 1);
-                read(s + 1, 0, 0);
+                __builtin_amdgcn_sched_barrier(0);
+                load_some(phase_of(phase * PB + i, PB * STEPS), phase_of(phase * PB + i + 1, PB * STEPS));
+                    __builtin_amdgcn_sched_barrier(0);
             }
-            products(1);
+        };
+        read(0, 0);
+        // (the first slab's phases but the last, which is the first one's behind next())
+        load_some(0, phase_of(PB, PB * STEPS));
+        for (int s = 0; s < slabs; ++s) {
+#pragma unroll
+            for (int st = 0; st < STEPS; ++st) {
+                if (st + 1 < STEPS) {
+                    read(st + 1, (st + 1) & 1);
+                } else if (s + 1 < slabs) {
+                    next(s + 1);
+                    read(0, 0);
+                }
+                products(st & 1, (st + 1) % STEPS);
+            }
         }
     } else {
         for (int s = 0; s < slabs; ++s) {
@@ -461,8 +558,8 @@ __global__ void __launch_bounds__(WM* WN * 64, WM* WN == 4 ? 2 : 1) matmul_block
                 sp[i] = ((MAT_CONST(float)*)(uintptr_t)a.p_scale[part_of(i)])[col / kScaleBlock * a.scale_cols + s];
             }
 #pragma unroll
-            for (int h = 0; h < QB; ++h) sq[h] = *(const float*)(q_slab(s) + S::Q_BYTES + S::P_BYTES + ((wm * QB + h) * 32 + j) * 4);
-            auto add = [&](int i, int h, const mf32x16& c) {
+            for (int h = 0; h < QB; ++h) sq[h] = *(const float*)(q_slab(stage) + S::Q_BYTES + S::P_BYTES + ((wm * QB + h) * 32 + j) * 4);
+            auto add = [&](int i, int h, const mf32x16& c) MAT_INLINE {
                 const float f = sp[i] * sq[h];
 #pragma unroll
                 for (int v = 0; v < 16; ++v) acc[i][h][v] = __builtin_fmaf(c[v], f, acc[i][h][v]);
@@ -471,21 +568,21 @@ __global__ void __launch_bounds__(WM* WN * 64, WM* WN == 4 ? 2 : 1) matmul_block
             };
             if constexpr (DT == FEED_E4M3) {
                 // (one address for each of the four chunks and operand, the blocks at constant distances: more and the sums spill)
-                const uint32_t qa = lds_address(q_slab(s)) + (wm * QB * 32 + j) * kSlab, pa = lds_address(q_slab(s)) + S::Q_BYTES + (block_of(0) * 32 + j) * kSlab;
+                const uint32_t qa = lds_address(q_slab(stage)) + (wm * QB * 32 + j) * SLAB, pa = lds_address(q_slab(stage)) + S::Q_BYTES + (block_of(0) * 32 + j) * SLAB;
                 uint32_t chunk[4];
 #pragma unroll
-                for (int x = 0; x < 4; ++x) chunk[x] = ((2 * x + g) ^ (j & 7)) * 16;
+                for (int x = 0; x < 4; ++x) chunk[x] = ((2 * x + g) ^ chunk_turn(SLAB, j)) * 16;
                 auto chunk_at = [](uint32_t at, int more) { return *(MAT_LDS(const mu32x4)*)((MAT_LDS(const char)*)(uintptr_t)at + more); };
                 mu32x4 pv[PB][2][2], qv[2][2];
-                auto read_q = [&](int h) {
+                auto read_q = [&](int h) MAT_INLINE {
 #pragma unroll
-                    for (int x = 0; x < 4; ++x) qv[x / 2][x % 2] = chunk_at(qa + chunk[x], h * 32 * kSlab);
+                    for (int x = 0; x < 4; ++x) qv[x / 2][x % 2] = chunk_at(qa + chunk[x], h * 32 * SLAB);
                 };
 #pragma unroll
                 for (int i = 0; i < PB; ++i)
 #pragma unroll
                     for (int x = 0; x < 4; ++x)
-                        pv[i][x / 2][x % 2] = chunk_at(pa + chunk[x], (part_of(i) * S::P_ROWS + (block_of(i) - block_of(0)) * 32) * kSlab);
+                        pv[i][x / 2][x % 2] = chunk_at(pa + chunk[x], (part_of(i) * S::P_ROWS + (block_of(i) - block_of(0)) * 32) * SLAB);
                 read_q(0);
 #pragma unroll
                 for (int h = 0; h < QB; ++h) {
@@ -499,6 +596,7 @@ __global__ void __launch_bounds__(WM* WN * 64, WM* WN == 4 ? 2 : 1) matmul_block
                     }
                     __builtin_amdgcn_sched_barrier(0);
                     if (h + 1 < QB) read_q(h + 1);
+                    load_some(phase_of((h + 1) % QB, QB), phase_of((h + 1) % QB + 1, QB));
 #pragma unroll
                     for (int i = 0; i < PB; ++i) add(i, h, c[i]);
                     __builtin_amdgcn_sched_barrier(0);
@@ -515,9 +613,9 @@ __global__ void __launch_bounds__(WM* WN * 64, WM* WN == 4 ? 2 : 1) matmul_block
                 for (int x = 0; x < 4; ++x) {
                     mu32x4 pv[PB], qv[QB];
 #pragma unroll
-                    for (int i = 0; i < PB; ++i) pv[i] = read_block<1, false, S::P_ROWS>(p_slab(s, i), block_of(i), x, lane);
+                    for (int i = 0; i < PB; ++i) pv[i] = read_block<1, false, S::P_ROWS, SLAB>(p_slab(stage, i), block_of(i), x, lane);
 #pragma unroll
-                    for (int h = 0; h < QB; ++h) qv[h] = read_block<1, false, S::BM>(q_slab(s), wm * QB + h, x, lane);
+                    for (int h = 0; h < QB; ++h) qv[h] = read_block<1, false, S::BM, SLAB>(q_slab(stage), wm * QB + h, x, lane);
 #pragma unroll
                     for (int half = 0; half < 2; ++half)
 #pragma unroll
@@ -529,11 +627,15 @@ __global__ void __launch_bounds__(WM* WN * 64, WM* WN == 4 ? 2 : 1) matmul_block
                 for (int i = 0; i < PB; ++i)
 #pragma unroll
                     for (int h = 0; h < QB; ++h) add(i, h, c[i][h]);
-                if (s + 1 < slabs) next(s + 1);
+                if (s + 1 < slabs) {
+                    next(s + 1);
+                    load_some(0, LOADS);
+                }
             }
         }
     }
 
+    loads_done();                                              // (also those of zeros: LDS is handed on when the workgroup ends)
 #pragma unroll
     for (int h = 0; h < QB; ++h) {
         const int64_t m = m0 + (wm * QB + h) * 32 + j;
@@ -548,12 +650,186 @@ __global__ void __launch_bounds__(WM* WN * 64, WM* WN == 4 ? 2 : 1) matmul_block
     }
 }
 
-template <int DT, int FORM, int QB, int PB, int WM, int WN, bool QD, bool PD>
-static int launch_block(FeedArgs a, void* stream) {
-    using S = BlockShape<DT, FORM, QB, PB, WM, WN>;
-    auto kernel = matmul_block_kernel<DT, FORM, QB, PB, WM, WN, QD, PD>;
+// Few rows: the weights set the pace, and there are more compute units than tiles of the kernel above.  A workgroup owns QB x PB blocks of 32 x 32 of Out and
+// its four waves divide the contraction, every fourth slab each; a wave brings its slabs to LDS and multiplies them alone, so that nothing waits at a
+// barrier, and the four sums are added at the end, in the order of the waves.  DEPTH slabs of a wave are in LDS or on their way.
+template <int DT, int FORM, int QB, int PB>
+struct WaveShape {
+    static constexpr int ESZ = feed_size(DT), BM = QB * 32;
+    static constexpr bool GATED = FORM == FEED_GATED, Q_STRIDED = FORM == FEED_BOTH, P_STRIDED = FORM >= FEED_RIGHT;
+    static constexpr int P_PARTS = GATED ? 2 : 1, P_ROWS = PB * 32 / P_PARTS, COLS = P_ROWS;
+    static constexpr int SLAB = 128, Q_BYTES = BM * SLAB, P_BYTES = PB * 32 * SLAB, STAGE = Q_BYTES + P_BYTES + (ESZ == 1 ? 256 : 0);
+    static constexpr int LOADS = (QB + PB) * 4 + (ESZ == 1 ? 1 : 0);            // of a slab
+    static constexpr int FIT = 160 * 1024 / (4 * STAGE), DEPTH = FIT < 4 ? FIT : 4, LDS = 4 * DEPTH * STAGE;
+    static_assert(DEPTH >= 2 && (DEPTH - 1) * LOADS < 64 && LDS >= 4 * QB * PB * 4096, "a wave's slabs, and the sums at the end");
+};
+
+template <int DT, int FORM, int QB, int PB, bool QD, bool PD>
+__global__ void __launch_bounds__(256) matmul_waves_kernel(const FeedArgs a) {
+    using S = WaveShape<DT, FORM, QB, PB>;
+    constexpr int ESZ = S::ESZ, SLAB = S::SLAB, KE = SLAB / ESZ, DEPTH = QD && PD ? S::DEPTH : 2;
+    extern __shared__ __align__(16) char s_mem[];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int j = lane & 31, g = lane >> 5;
+    const TilePlace at = tile_place(a, blockIdx.x);
+    const int64_t m0 = (int64_t)at.m * S::BM, n0 = (int64_t)at.n * S::COLS;
+    char* const mine = s_mem + wave * (S::DEPTH * S::STAGE);
+
+    Loader<ESZ, S::Q_STRIDED, S::BM, 1, SLAB, QD> q;
+    Loader<ESZ, S::P_STRIDED, S::P_ROWS, 1, SLAB, PD> p[S::P_PARTS];
+    q.init(a.q[at.product], m0, 0, lane);
+#pragma unroll
+    for (int h = 0; h < S::P_PARTS; ++h) p[h].init(a.p[h], n0, 0, lane);
+    const int per_segment = (int)((a.q[0].k + KE - 1) / KE), slabs = per_segment * a.segments, turns = (slabs + 3) / 4;
+    const i32x4 scales = ESZ == 1 ? bytes_from((const char*)(a.q_scale + m0 * a.scale_cols), min((int64_t)S::BM, a.M - m0) * a.scale_cols * 4) : i32x4{0, 0, 0, 0};
+    const uint32_t scale_off = (uint32_t)lane * a.scale_cols * 4;
+    int segment = 0;
+    // the wave's slab of turn `i` into stage `stage`; none behind the last: zeros, so that the loads on their way can be counted
+    auto begin = [&](int i, int stage) MAT_INLINE {
+        const int s = i * 4 + wave;
+        const uint32_t to = lds_address(mine) + stage * S::STAGE;
+        int x = s;
+        if constexpr (FORM == FEED_RIGHT)
+            if (s >= per_segment) {
+                x = s - per_segment;
+                if (segment == 0 && a.segments > 1) {
+                    segment = 1;
+                    q.move(a.q[1], m0);
+                    p[0].move(a.p[1], n0);
+                }
+            }
+        q.prepare(x, s < slabs);
+#pragma unroll
+        for (int l = 0; l < S::BM / 8; ++l) q.issue(l, to);
+#pragma unroll
+        for (int h = 0; h < S::P_PARTS; ++h) {
+            p[h].prepare(x, s < slabs);
+#pragma unroll
+            for (int l = 0; l < S::P_ROWS / 8; ++l) p[h].issue(l, to + S::Q_BYTES + h * S::P_ROWS * SLAB);
+        }
+        if constexpr (ESZ == 1) load_word_to_lds_unseen(scales, scale_off + x * 4, to + S::Q_BYTES + S::P_BYTES);
+    };
+    auto put = [&](int stage) MAT_INLINE {
+        char* const to = mine + stage * S::STAGE;
+        q.put(to);
+#pragma unroll
+        for (int h = 0; h < S::P_PARTS; ++h) p[h].put(to + S::Q_BYTES + h * S::P_ROWS * SLAB);
+    };
+    auto part_of = [&](int i) { return S::GATED ? i / (PB / 2) : 0; };
+    auto block_of = [&](int i) { return S::GATED ? i % (PB / 2) : i; };
+
+    mf32x16 acc[PB][QB];
+#pragma unroll
+    for (int i = 0; i < PB; ++i)
+#pragma unroll
+        for (int h = 0; h < QB; ++h)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) acc[i][h][v] = 0.f;
+    auto compute = [&](int s, int stage) MAT_INLINE {
+        const char* const qs = mine + stage * S::STAGE;
+        const char* const ps = qs + S::Q_BYTES;
+        mu32x4 pv[4][PB], qv[4][QB];
+#pragma unroll
+        for (int st = 0; st < 4; ++st) {
+#pragma unroll
+            for (int i = 0; i < PB; ++i) pv[st][i] = read_block<ESZ, S::P_STRIDED, S::P_ROWS, SLAB>(ps + part_of(i) * S::P_ROWS * SLAB, block_of(i), st, lane);
+#pragma unroll
+            for (int h = 0; h < QB; ++h) qv[st][h] = read_block<ESZ, S::Q_STRIDED, S::BM, SLAB>(qs, h, st, lane);
+        }
+        if constexpr (ESZ > 1) {
+#pragma unroll
+            for (int st = 0; st < 4; ++st)
+#pragma unroll
+                for (int i = 0; i < PB; ++i)
+#pragma unroll
+                    for (int h = 0; h < QB; ++h) multiply<DT>(acc[i][h], pv[st][i], qv[st][h]);
+        } else {
+            float sq[QB];
+#pragma unroll
+            for (int h = 0; h < QB; ++h) sq[h] = *(const float*)(ps + S::P_BYTES + (h * 32 + j) * 4);
+#pragma unroll
+            for (int i = 0; i < PB; ++i) {
+                const int64_t col = min(n0 + block_of(i) * 32, a.N - 1);
+                const float sp = ((MAT_CONST(float)*)(uintptr_t)a.p_scale[part_of(i)])[col / kScaleBlock * a.scale_cols + s];
+#pragma unroll
+                for (int h = 0; h < QB; ++h) {
+                    mf32x16 c;
+#pragma unroll
+                    for (int v = 0; v < 16; ++v) c[v] = 0.f;
+                    if constexpr (DT == FEED_E4M3) {
+#pragma unroll
+                        for (int x = 0; x < 2; ++x)
+                            c = multiply_e4m3(c, {pv[2 * x][i], pv[2 * x + 1][i]}, {qv[2 * x][h], qv[2 * x + 1][h]});
+                    } else {
+#pragma unroll
+                        for (int x = 0; x < 8; ++x) multiply<FEED_BF16>(c, half_as_bf16(pv[x / 2][i], x % 2), half_as_bf16(qv[x / 2][h], x % 2));
+                    }
+                    const float f = sp * sq[h];
+#pragma unroll
+                    for (int v = 0; v < 16; ++v) acc[i][h][v] = __builtin_fmaf(c[v], f, acc[i][h][v]);
+                }
+            }
+        }
+    };
+
+    if constexpr (QD && PD) {
+#pragma unroll
+        for (int i = 0; i < DEPTH - 1; ++i) begin(i, i);
+        int stage = 0, free = DEPTH - 1;
+        for (int i = 0; i < turns; ++i) {
+            lds_done();                                    // what was read of the stage that is filled now
+            begin(i + DEPTH - 1, free);
+            asm volatile("s_waitcnt vmcnt(%0)" ::"n"((DEPTH - 1) * S::LOADS) : "memory");
+            if (i * 4 + wave < slabs) compute(i * 4 + wave, stage);
+            free = stage;
+            stage = stage + 1 == DEPTH ? 0 : stage + 1;
+        }
+    } else {
+        begin(0, 0);
+        loads_done();
+        put(0);
+        for (int i = 0; i < turns; ++i) {
+            lds_done();
+            begin(i + 1, (i + 1) & 1);
+            asm volatile("" ::: "memory");
+            if (i * 4 + wave < slabs) compute(i * 4 + wave, i & 1);
+            loads_done();
+            put((i + 1) & 1);
+        }
+    }
+    loads_done();
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < PB; ++i)
+#pragma unroll
+        for (int h = 0; h < QB; ++h)
+#pragma unroll
+            for (int v = 0; v < 4; ++v)
+                *(mf32x4*)(s_mem + ((((wave * PB + i) * QB + h) * 4 + v) * 64 + lane) * 16) =
+                    mf32x4{acc[i][h][v * 4], acc[i][h][v * 4 + 1], acc[i][h][v * 4 + 2], acc[i][h][v * 4 + 3]};
+    __syncthreads();
+    // wave w finishes the w-th four of every eight columns
+    auto sum = [&](int i, int h) {
+        mf32x4 t = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            const mf32x4 x = *(const mf32x4*)(s_mem + ((((w * PB + i) * QB + h) * 4 + wave) * 64 + lane) * 16);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) t[e] = w == 0 ? x[e] : t[e] + x[e];
+        }
+        return t;
+    };
+#pragma unroll
+    for (int h = 0; h < QB; ++h)
+#pragma unroll
+        for (int i = 0; i < (S::GATED ? PB / 2 : PB); ++i)
+            finish_four<DT, S::GATED>(a, at.product, m0 + h * 32 + j, n0 + block_of(i) * 32 + wave * 8 + g * 4, sum(i, h), sum(S::GATED ? i + PB / 2 : i, h));
+}
+
+// One launch of a kernel whose workgroups own S::BM x S::COLS of Out
+template <class S>
+static int launch_tiles(void (*kernel)(const FeedArgs), OncePerDevice& once, FeedArgs a, int threads, void* stream) {
     if constexpr (S::LDS > 64 * 1024) {
-        static OncePerDevice once;
         int device = -1;
         if (hipGetDevice(&device) != hipSuccess || !once(device, [&] {
                 return hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024) == hipSuccess;
@@ -566,22 +842,73 @@ static int launch_block(FeedArgs a, void* stream) {
     // (a gradient's columns go on to the end of its rows in the workspace)
     a.tiles_n = (int32_t)(((S::GATED && a.grad_out ? a.grad_cols : a.N) + S::COLS - 1) / S::COLS);
     a.n_tiles = a.tiles_m * a.tiles_n * a.products;
-    hipLaunchKernelGGL(kernel, dim3(a.n_tiles), dim3(S::WAVES * 64), S::LDS, (hipStream_t)stream, a);
+    hipLaunchKernelGGL(kernel, dim3(a.n_tiles), dim3(threads), S::LDS, (hipStream_t)stream, a);
     return hipGetLastError() == hipSuccess ? 0 : 1;
+}
+template <int DT, int FORM, int QB, int PB, int WM, int WN, int SLAB, int STAGES, bool QD, bool PD>
+static int launch_block(const FeedArgs& a, void* stream) {
+    static OncePerDevice once;
+    return launch_tiles<BlockShape<DT, FORM, QB, PB, WM, WN, SLAB, STAGES>>(matmul_block_kernel<DT, FORM, QB, PB, WM, WN, SLAB, STAGES, QD, PD>, once, a,
+                                                                            WM * WN * 64, stream);
+}
+template <int DT, int FORM, int QB, int PB, bool QD, bool PD>
+static int launch_waves(const FeedArgs& a, void* stream) {
+    static OncePerDevice once;
+    return launch_tiles<WaveShape<DT, FORM, QB, PB>>(matmul_waves_kernel<DT, FORM, QB, PB, QD, PD>, once, a, 256, stream);
 }
 
 // Whether an operand can go straight to LDS
 static bool direct(const FeedOperand& o, int size, bool strided) {
     return reinterpret_cast<uintptr_t>(o.base) % 16 == 0 && o.ld % 16 == 0 && (o.padded || (strided ? o.rows : o.k) * size % 16 == 0);
 }
-static int64_t tiles(const FeedArgs& a, int64_t rows, int64_t cols) { return (a.M + rows - 1) / rows * ((a.N + cols - 1) / cols) * a.products; }
+// Which kernel: the one with the least estimated time.  A workgroup of 256 or 512 threads has a compute unit to itself (two of the 128 x 128 tiles with two
+// stages share one), a launch runs in rounds of 256, and a round takes 3 us and what a slab of 128 bytes (the dividing waves: four slabs, one each) was
+// measured to take, in us, on shapes of 64 to 8192 rows:
+//                                   bf16, 8 bits    fp32 (bound by its matrix instructions)
+//     32 x 32 divided (gated: 32 x 2 x 32)   0.75 (1.15)     0.8 (1.2)
+//     64 x 32 divided (gated: 64 x 2 x 32)   1.15 (1.25)     1.2 (1.9)
+//     64 x 64 divided                        1.45            1.9
+//     128 x 128, four stages                 0.85            1.9
+//     128 x 128, two of two stages           1.6             3.8
+//     256 x 256                              2.0             -
+// Examples, us, the chosen kernel first: 8 bits (64, 8192, 4096) 15 on 32 x 32, 22 on 64 x 32; (256, 4096, 4096) 15.5 on 64 x 64, 22 on 64 x 32; (1024, 4096, 4096)
+// 34 on 128 x 128 with four stages, 39 with two, 47 on 64 x 64; (2048, 4096, 4096) 51 with two stages, 64 with four, 78 on 256 x 256.
+struct Estimate {
+    double slabs;        // of 128 bytes
+    const FeedArgs* a;
+    double us(int64_t rows, int64_t cols, int waves, double slab_us, int per_unit = 1) const {
+        const int64_t t = (a->M + rows - 1) / rows * ((a->N + cols - 1) / cols) * a->products, at_once = 256 * per_unit;
+        return (double)((t + at_once - 1) / at_once) * (3.0 + std::ceil(slabs / waves) * slab_us);
+    }
+};
 
 template <int DT, int FORM, bool QD, bool PD>
 static int launch_shape(const FeedArgs& a, void* stream) {
-    constexpr bool LARGE = QD && PD && (DT == FEED_BF16 || DT == FEED_E4M3);
-    if constexpr (LARGE)
-        if (tiles(a, 256, FORM == FEED_GATED ? 128 : 256) >= 192) return launch_block<DT, FORM, 4, 2, 2, 4, QD, PD>(a, stream);
-    return launch_block<DT, FORM, 2, 2, 2, 2, QD, PD>(a, stream);
+    constexpr bool F32 = DT == FEED_F32, GATED = FORM == FEED_GATED, DIRECT = QD && PD;
+    constexpr int HALF = GATED ? 2 : 1;
+    const Estimate e = {(double)a.q[0].k * feed_size(DT) / 128 * a.segments, &a};
+    constexpr double AHEAD = DIRECT ? 1.0 : 2.0;         // (through registers a dividing wave is one slab ahead)
+    double least = e.us(32, 32, 4, AHEAD * (GATED ? 1.15 : F32 ? 0.8 : 0.75));
+    int best = 0;
+    auto candidate = [&](int kernel, double us) {
+        if (us < least) least = us, best = kernel;
+    };
+    candidate(1, e.us(64, 32, 4, AHEAD * (GATED ? (F32 ? 1.9 : 1.25) : F32 ? 1.2 : 1.15)));
+    if constexpr (!GATED) candidate(2, e.us(64, 64, 4, AHEAD * (F32 ? 1.9 : 1.45)));
+    if constexpr (DIRECT) candidate(3, e.us(128, 128 / HALF, 1, F32 ? 1.9 : 0.85));
+    candidate(4, e.us(128, 128 / HALF, 1, F32 ? 3.8 : 1.6, 2));
+    if constexpr (DIRECT && (DT == FEED_BF16 || DT == FEED_E4M3)) candidate(5, e.us(256, 256 / HALF, 1, 2.0));
+    if (best == 0) return launch_waves<DT, FORM, 1, HALF, QD, PD>(a, stream);
+    if (best == 1) return launch_waves<DT, FORM, 2, HALF, QD, PD>(a, stream);
+    if constexpr (!GATED)
+        if (best == 2) return launch_waves<DT, FORM, 2, 2, QD, PD>(a, stream);
+    if constexpr (DIRECT)
+        if (best == 3) return launch_block<DT, FORM, 2, 2, 2, 2, 128, 4, QD, PD>(a, stream);
+    if constexpr (DIRECT && DT == FEED_BF16)
+        if (best == 5) return launch_block<DT, FORM, 4, 2, 2, 4, 64, 4, QD, PD>(a, stream);
+    if constexpr (DIRECT && DT == FEED_E4M3)
+        if (best == 5) return launch_block<DT, FORM, 4, 2, 2, 4, 128, 2, QD, PD>(a, stream);
+    return launch_block<DT, FORM, 2, 2, 2, 2, 128, 2, QD, PD>(a, stream);
 }
 template <int DT, int FORM>
 static int launch_form(const FeedArgs& a, void* stream) {
