@@ -29,9 +29,8 @@ bool element_type(int dtype) { return dtype == CACNN_F32 || dtype == CACNN_BF16_
 FeedOperand operand(const void* p, int64_t ld, int size, int64_t rows, int64_t k, bool padded = false) {
     return {static_cast<const char*>(p), ld * size, k, rows, padded};
 }
-// an output whose groups of four columns start at multiples of their size leaves in wide stores
 FeedOut output(void* p, int64_t ld, int size) {
-    return {static_cast<char*>(p), ld * size, size, multiple(p, 4 * size) && ld % 4 == 0};
+    return {static_cast<char*>(p), ld * size, size, multiple(p, 16) && ld * size % 16 == 0 ? 2 : multiple(p, 4 * size) && ld % 4 == 0};
 }
 
 int64_t padded(int64_t F) { return (F + 63) / 64 * 64; }      // columns of a row in the workspace

@@ -30,7 +30,8 @@ struct FeedOperand {
     bool padded;     // zeros follow each row's elements up to a multiple of 16 bytes
 };
 
-// An output array of rows x cols elements of `size` bytes; wide: a lane's four columns leave in one store where all four exist
+// An output array of rows x cols elements of `size` bytes; wide: 1 where every fourth column starts at a multiple of four elements' bytes, so that four leave in one
+// store, 2 where rows start at multiples of 16 bytes
 struct FeedOut {
     char* base;
     int64_t ld;      // bytes

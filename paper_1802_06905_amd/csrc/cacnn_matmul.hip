@@ -313,63 +313,71 @@ __device__ __forceinline__ uint32_t two_bf16(float lo, float hi) {
     return (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)lo) | (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)hi) << 16;
 }
 
-// Columns n .. n + 3 of row m, those below `cols`
-template <int DT>
-__device__ __forceinline__ void store_four(const FeedOut& o, int64_t m, int64_t n, int64_t cols, mf32x4 v) {
-    constexpr bool words = DT == FEED_F32 || DT == FEED_E4M3_EXACT;
-    char* const p = o.base + m * o.ld + n * (words ? 4 : 2);
-    const mu32x2 packed = {two_bf16(v[0], v[1]), two_bf16(v[2], v[3])};
-    if (o.wide && n + 4 <= cols) {
-        if (words) *(mf32x4*)p = v;
-        else *(mu32x2*)p = packed;
+// E adjacent columns from n on of row m, those below `cols`: 16 or 8 bytes
+template <int DT, int E>
+__device__ __forceinline__ void store_run(const FeedOut& o, int64_t m, int64_t n, int64_t cols, const float (&v)[E]) {
+    constexpr bool WORDS = DT == FEED_F32 || DT == FEED_E4M3_EXACT;
+    static_assert(E == 4 || (E == 8 && !WORDS), "what one store takes");
+    char* const p = o.base + m * o.ld + n * (WORDS ? 4 : 2);
+    if ((E * (WORDS ? 4 : 2) == 16 ? o.wide == 2 : o.wide != 0) && n + E <= cols) {
+        if constexpr (WORDS) *(mf32x4*)p = mf32x4{v[0], v[1], v[2], v[3]};
+        else if constexpr (E == 4) *(mu32x2*)p = mu32x2{two_bf16(v[0], v[1]), two_bf16(v[2], v[3])};
+        else *(mu32x4*)p = mu32x4{two_bf16(v[0], v[1]), two_bf16(v[2], v[3]), two_bf16(v[4], v[5]), two_bf16(v[6], v[7])};
     } else {
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
+        for (int e = 0; e < E; ++e)
             if (n + e < cols) {
-                if (words) ((float*)p)[e] = v[e];
-                else ((uint16_t*)p)[e] = (uint16_t)(packed[e / 2] >> (e % 2 * 16));
+                if constexpr (WORDS) ((float*)p)[e] = v[e];
+                else ((uint16_t*)p)[e] = __builtin_bit_cast(uint16_t, (__bf16)v[e]);
             }
     }
 }
 
-// What is done with four adjacent columns of a row: sums of the plain products, or of gate and up
-template <int DT, bool GATED>
-__device__ __forceinline__ void finish_four(const FeedArgs& a, int product, int64_t m, int64_t n, mf32x4 v, mf32x4 u) {
+// What becomes of E adjacent columns of a row, given their sums (gated: v of gate, u of up)
+template <int DT, bool GATED, int E>
+__device__ __forceinline__ void finish_run(const FeedArgs& a, int product, int64_t m, int64_t n, const float (&v)[E], const float (&u)[E]) {
     if (m >= a.M) return;
     if constexpr (!GATED) {
-        store_four<DT>(a.out[product], m, n, a.N, v);
+        store_run<DT>(a.out[product], m, n, a.N, v);
     } else if (feed_size(DT) > 1 && a.grad_out) {
         if (n >= a.grad_cols) return;
-        mf32x4 d = {0.f, 0.f, 0.f, 0.f};
+        float d[E];
         const char* const p = a.grad_out + m * a.grad_out_ld + n * feed_size(DT);
-        if (a.grad_out_wide && n + 4 <= a.N) {
-            if constexpr (DT == FEED_F32) {
-                d = *(const mf32x4*)p;
-            } else {
-                const mu32x2 w = *(const mu32x2*)p;
-                d = mf32x4{__uint_as_float(w[0] << 16), __uint_as_float(w[0] & 0xffff0000u), __uint_as_float(w[1] << 16), __uint_as_float(w[1] & 0xffff0000u)};
+        if (a.grad_out_wide && n + E <= a.N) {
+#pragma unroll
+            for (int e = 0; e < E; e += 4) {
+                if constexpr (DT == FEED_F32) {
+                    const mf32x4 w = *(const mf32x4*)(p + e * 4);
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) d[e + x] = w[x];
+                } else {
+                    const mu32x2 w = *(const mu32x2*)(p + e * 2);
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) d[e + x] = __uint_as_float(x & 1 ? w[x / 2] & 0xffff0000u : w[x / 2] << 16);
+                }
             }
         } else {
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-                if (n + e < a.N) d[e] = DT == FEED_F32 ? ((const float*)p)[e] : __uint_as_float((uint32_t)((const uint16_t*)p)[e] << 16);
+            for (int e = 0; e < E; ++e)
+                d[e] = n + e >= a.N ? 0.f : DT == FEED_F32 ? ((const float*)p)[e] : __uint_as_float((uint32_t)((const uint16_t*)p)[e] << 16);
         }
-        mf32x4 dg, du;
+        float dg[E], du[E];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            float g = 0.f, h = 0.f;
-            if (n + e < a.N) gate_grad(a.activation, v[e], u[e], d[e], g, h);
-            dg[e] = g, du[e] = h;
+        for (int e = 0; e < E; ++e) {
+            dg[e] = du[e] = 0.f;
+            if (n + e < a.N) gate_grad(a.activation, v[e], u[e], d[e], dg[e], du[e]);
         }
-        store_four<DT>(a.out[0], m, n, a.grad_cols, dg);
-        store_four<DT>(a.out[1], m, n, a.grad_cols, du);
+        store_run<DT>(a.out[0], m, n, a.grad_cols, dg);
+        store_run<DT>(a.out[1], m, n, a.grad_cols, du);
     } else {
-        mf32x4 h;
+        float h[E];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) h[e] = gate_value(a.activation, v[e]) * u[e];
-        store_four<DT>(a.out[0], m, n, a.N, h);
-        if (a.gate_out.base) store_four<DT>(a.gate_out, m, n, a.N, v);
-        if (a.up_out.base) store_four<DT>(a.up_out, m, n, a.N, u);
+        for (int e = 0; e < E; ++e) h[e] = gate_value(a.activation, v[e]) * u[e];
+        store_run<DT>(a.out[0], m, n, a.N, h);
+        if (a.gate_out.base) {
+            store_run<DT>(a.gate_out, m, n, a.N, v);
+            store_run<DT>(a.up_out, m, n, a.N, u);
+        }
     }
 }
 
@@ -635,18 +643,36 @@ __global__ void __launch_bounds__(WM* WN * 64, WM* WN == 4 ? 2 : 1) matmul_block
         }
     }
 
-    loads_done();                                              // (also those of zeros: LDS is handed on when the workgroup ends)
+    // Out: a wave turns the sums of 32 rows round in its part of LDS, so that a lane has 16 bytes of a row, and several lanes the row's columns of the
+    // wave: stored from where the matrix instructions leave them, 16 bytes of a row at a time, results make four times as many pieces of lines.  (bf16 gated
+    // (8192, 4096, 8192) with gate and up kept, 400 MB of results: 1160 us that way.)
+    loads_done();                                              // (also those of zeros: their LDS is given up)
+    __syncthreads();
+    constexpr int RUN = DT == FEED_F32 || DT == FEED_E4M3_EXACT ? 4 : 8, COLS = (S::GATED ? PB / 2 : PB) * 32, PITCH = PB * 128 + 16, LANES = COLS / RUN;
+    static_assert(WAVES * 32 * PITCH <= S::LDS, "a block's rows for each wave");
+    char* const turn = s_mem + wave * (32 * PITCH);
 #pragma unroll
     for (int h = 0; h < QB; ++h) {
-        const int64_t m = m0 + (wm * QB + h) * 32 + j;
 #pragma unroll
-        for (int i = 0; i < (S::GATED ? PB / 2 : PB); ++i)
+        for (int i = 0; i < PB; ++i)
 #pragma unroll
-            for (int v = 0; v < 16; v += 4) {
-                const int64_t n = n0 + block_of(i) * 32 + v * 2 + g * 4;
-                const mf32x16 &x = acc[i][h], &y = acc[S::GATED ? i + PB / 2 : i][h];
-                finish_four<DT, S::GATED>(a, at.product, m, n, mf32x4{x[v], x[v + 1], x[v + 2], x[v + 3]}, mf32x4{y[v], y[v + 1], y[v + 2], y[v + 3]});
+            for (int v = 0; v < 16; v += 4)
+                *(mf32x4*)(turn + j * PITCH + (i * 32 + v * 2 + g * 4) * 4) = mf32x4{acc[i][h][v], acc[i][h][v + 1], acc[i][h][v + 2], acc[i][h][v + 3]};
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll 1
+        for (int row = lane / LANES; row < 32; row += 64 / LANES) {
+            const int col = lane % LANES * RUN;
+            float v[RUN], u[RUN];
+#pragma unroll
+            for (int e = 0; e < RUN; ++e) {
+                v[e] = *(const float*)(turn + row * PITCH + (col + e) * 4);
+                u[e] = S::GATED ? *(const float*)(turn + row * PITCH + (COLS + col + e) * 4) : 0.f;
             }
+            finish_run<DT, S::GATED>(a, at.product, m0 + (wm * QB + h) * 32 + row, n0 + block_of(0) * 32 + col, v, u);
+        }
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_wave_barrier();
     }
 }
 
@@ -809,21 +835,23 @@ __global__ void __launch_bounds__(256) matmul_waves_kernel(const FeedArgs a) {
                     mf32x4{acc[i][h][v * 4], acc[i][h][v * 4 + 1], acc[i][h][v * 4 + 2], acc[i][h][v * 4 + 3]};
     __syncthreads();
     // wave w finishes the w-th four of every eight columns
-    auto sum = [&](int i, int h) {
-        mf32x4 t = {0.f, 0.f, 0.f, 0.f};
+    auto sum = [&](int i, int h, float (&t)[4]) {
 #pragma unroll
         for (int w = 0; w < 4; ++w) {
             const mf32x4 x = *(const mf32x4*)(s_mem + ((((w * PB + i) * QB + h) * 4 + wave) * 64 + lane) * 16);
 #pragma unroll
             for (int e = 0; e < 4; ++e) t[e] = w == 0 ? x[e] : t[e] + x[e];
         }
-        return t;
     };
 #pragma unroll
     for (int h = 0; h < QB; ++h)
 #pragma unroll
-        for (int i = 0; i < (S::GATED ? PB / 2 : PB); ++i)
-            finish_four<DT, S::GATED>(a, at.product, m0 + h * 32 + j, n0 + block_of(i) * 32 + wave * 8 + g * 4, sum(i, h), sum(S::GATED ? i + PB / 2 : i, h));
+        for (int i = 0; i < (S::GATED ? PB / 2 : PB); ++i) {
+            float v[4], u[4];
+            sum(i, h, v);
+            sum(S::GATED ? i + PB / 2 : i, h, u);
+            finish_run<DT, S::GATED>(a, at.product, m0 + h * 32 + j, n0 + block_of(i) * 32 + wave * 8 + g * 4, v, u);
+        }
 }
 
 // One launch of a kernel whose workgroups own S::BM x S::COLS of Out
