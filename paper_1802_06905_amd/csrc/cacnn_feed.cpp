@@ -2,6 +2,7 @@
 #include <stdint.h>
 
 #include <algorithm>
+#include <climits>
 
 #include "../../include/cacnn.h"
 #include "cacnn_feed.h"
@@ -29,11 +30,20 @@ bool element_type(int dtype) { return dtype == CACNN_F32 || dtype == CACNN_BF16_
 FeedOperand operand(const void* p, int64_t ld, int size, int64_t rows, int64_t k, bool padded = false) {
     return {static_cast<const char*>(p), ld * size, k, rows, padded};
 }
-FeedOut output(void* p, int64_t ld, int size) {
-    return {static_cast<char*>(p), ld * size, size, multiple(p, 16) && ld * size % 16 == 0 ? 2 : multiple(p, 4 * size) && ld % 4 == 0};
-}
+FeedOut output(void* p, int64_t ld, int size) { return {static_cast<char*>(p), ld * size, size}; }
 
-int64_t padded(int64_t F) { return (F + 63) / 64 * 64; }      // columns of a row in the workspace
+int64_t padded(int64_t n) { return (n + 63) / 64 * 64; }      // columns of a row in the workspace
+
+// The workspace of the backward pass: the gradients of gate and up, and, where rows of C elements are no multiple of 16 bytes, X and both weights with rows
+// that are: the products read them two and three times each, and faster straight to LDS (bf16 (2048, 2047, 4095) 490 us in all without the copies, 289 with them).
+// Not for few rows, where the copies would be most of the traffic.
+struct Workspace {
+    int64_t ld_f, ld_c;            // elements of a row; ld_c 0: no copies
+    int64_t grad, x, w;            // bytes of grad_gate (and of grad_up), of the copies of X and of a weight
+    Workspace(const cacnn_gated_problem& p, int size)
+        : ld_f(padded(p.F)), ld_c(p.C * size % 16 && p.T >= 128 ? padded(p.C) : 0), grad(p.T * ld_f * size), x(p.T * ld_c * size), w(p.F * ld_c * size) {}
+    int64_t bytes() const { return 2 * grad + x + 2 * w; }
+};
 
 bool valid_gated(cacnn_gated_problem* p) {
     return rows(p->T) && columns(p->C) && columns(p->F) && stride(&p->ld_x, p->C) && stride(&p->ld_w, p->C) && stride(&p->ld_out, p->F) &&
@@ -62,7 +72,6 @@ int cacnn_quantize(const cacnn_quantize_problem* problem, int dtype, const void*
     a.q = static_cast<uint8_t*>(q), a.ld_q = p.ld_q, a.scale = scale;
     a.T = p.T, a.C = p.C;
     a.blocks = (int32_t)((p.C + kScaleBlock - 1) / kScaleBlock);
-    a.wide = multiple(x, 16) && a.ld_x % 16 == 0 && multiple(q, 8) && p.ld_q % 8 == 0;
     return launched(launch_quantize(a, dtype, (int)p.block_rows, hip_stream));
 }
 
@@ -140,7 +149,7 @@ int cacnn_gated_workspace(const cacnn_gated_problem* problem, int dtype, size_t*
     cacnn_gated_problem p = *problem;
     if (!element_type(dtype) || !activation(p.activation)) return CACNN_ERR_UNSUPPORTED;
     if (!valid_gated(&p)) return CACNN_ERR_INVALID_ARG;
-    *bytes = (size_t)(2 * p.T * padded(p.F)) * feed_size(dtype);
+    *bytes = (size_t)Workspace(p, feed_size(dtype)).bytes();
     return CACNN_OK;
 }
 
@@ -155,12 +164,26 @@ int cacnn_gated_backward(const cacnn_gated_problem* problem, int dtype, const vo
     const int size = feed_size(dtype);
     for (const void* q : {x, w_gate, w_up, gate, up, grad_out, (const void*)grad_x, (const void*)grad_w_gate, (const void*)grad_w_up})
         if (!multiple(q, size)) return CACNN_ERR_INVALID_ARG;
-    const int64_t ld = padded(p.F);
-    if (!multiple(workspace, 16) || workspace_bytes / size / 2 < (size_t)(p.T * ld)) return CACNN_ERR_INVALID_ARG;
+    const Workspace ws(p, size);
+    if (!multiple(workspace, 16) || (int64_t)std::min(workspace_bytes, (size_t)INT64_MAX) < ws.bytes()) return CACNN_ERR_INVALID_ARG;
     if (!device_present()) return CACNN_ERR_NO_DEVICE;
+    const int64_t ld = ws.ld_f;
     // the gradients of the two products, in the workspace with rows padded by zeros
     char* const grad_gate = static_cast<char*>(workspace);
-    char* const grad_up = grad_gate + p.T * ld * size;
+    char* const grad_up = grad_gate + ws.grad;
+    if (ws.ld_c && p.T != 0) {
+        char* const copies = grad_up + ws.grad;
+        PadArgs a = {};
+        a.from[0] = static_cast<const char*>(x), a.from[1] = static_cast<const char*>(w_gate), a.from[2] = static_cast<const char*>(w_up);
+        a.ld_from[0] = p.ld_x * size, a.ld_from[1] = a.ld_from[2] = p.ld_w * size;
+        // (what is read: X where the products are computed again or a weight's gradient is wanted, the weights where X's is)
+        a.rows[0] = !gate || grad_w_gate ? p.T : 0, a.rows[1] = a.rows[2] = !gate || grad_x ? p.F : 0;
+        a.to = copies + (a.rows[0] ? 0 : ws.x), a.bytes = p.C * size, a.ld = ws.ld_c * size, a.size = size;
+        if (launch_pad(a, hip_stream) != 0) return CACNN_ERR_LAUNCH;
+        x = copies, w_gate = copies + ws.x, w_up = copies + ws.x + ws.w;
+        p.ld_x = p.ld_w = ws.ld_c;
+    }
+    const bool copied = ws.ld_c != 0;
     if (p.T != 0) {
         if (gate) {
             GateArgs a = {};
@@ -169,19 +192,17 @@ int cacnn_gated_backward(const cacnn_gated_problem* problem, int dtype, const vo
             a.grad_gate = grad_gate, a.grad_up = grad_up, a.ld = ld * size;
             a.T = p.T, a.F = p.F, a.cols = ld;
             a.activation = (int32_t)p.activation;
-            a.wide = multiple(gate, 16) && multiple(up, 16) && multiple(grad_out, 16) && a.ld_pre % 16 == 0 && a.ld_out % 16 == 0;
             if (launch_gate_grad(a, dtype, hip_stream) != 0) return CACNN_ERR_LAUNCH;
         } else {
             FeedArgs a = {};
             a.segments = a.products = 1;
-            a.q[0] = operand(x, p.ld_x, size, p.T, p.C);
-            a.p[0] = operand(w_gate, p.ld_w, size, p.F, p.C);
-            a.p[1] = operand(w_up, p.ld_w, size, p.F, p.C);
+            a.q[0] = operand(x, p.ld_x, size, p.T, p.C, copied);
+            a.p[0] = operand(w_gate, p.ld_w, size, p.F, p.C, copied);
+            a.p[1] = operand(w_up, p.ld_w, size, p.F, p.C, copied);
             a.out[0] = output(grad_gate, ld, size), a.out[1] = output(grad_up, ld, size);
             a.M = p.T, a.N = p.F;
             a.activation = (int32_t)p.activation;
             a.grad_out = static_cast<const char*>(grad_out), a.grad_out_ld = p.ld_out * size;
-            a.grad_out_wide = multiple(grad_out, 4 * size) && p.ld_out % 4 == 0;
             a.grad_cols = (int32_t)ld;
             if (launch_matmul(a, FEED_GATED, dtype, hip_stream) != 0) return CACNN_ERR_LAUNCH;
         }
@@ -190,7 +211,7 @@ int cacnn_gated_backward(const cacnn_gated_problem* problem, int dtype, const vo
         FeedArgs a = {};
         a.segments = 2, a.products = 1;
         a.q[0] = operand(grad_gate, ld, size, p.T, p.F, true), a.q[1] = operand(grad_up, ld, size, p.T, p.F, true);
-        a.p[0] = operand(w_gate, p.ld_w, size, p.C, p.F), a.p[1] = operand(w_up, p.ld_w, size, p.C, p.F);
+        a.p[0] = operand(w_gate, p.ld_w, size, p.C, p.F, copied), a.p[1] = operand(w_up, p.ld_w, size, p.C, p.F, copied);
         a.out[0] = output(grad_x, p.ld_grad_x, size);
         a.M = p.T, a.N = p.C;
         if (launch_matmul(a, FEED_RIGHT, dtype, hip_stream) != 0) return CACNN_ERR_LAUNCH;
@@ -199,7 +220,7 @@ int cacnn_gated_backward(const cacnn_gated_problem* problem, int dtype, const vo
         FeedArgs a = {};
         a.segments = 1, a.products = 2;
         a.q[0] = operand(grad_gate, ld, size, p.F, p.T, true), a.q[1] = operand(grad_up, ld, size, p.F, p.T, true);
-        a.p[0] = operand(x, p.ld_x, size, p.C, p.T);
+        a.p[0] = operand(x, p.ld_x, size, p.C, p.T, copied);
         a.out[0] = output(grad_w_gate, p.ld_grad_w, size), a.out[1] = output(grad_w_up, p.ld_grad_w, size);
         a.M = p.F, a.N = p.C;
         if (launch_matmul(a, FEED_BOTH, dtype, hip_stream) != 0) return CACNN_ERR_LAUNCH;

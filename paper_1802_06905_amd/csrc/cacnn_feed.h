@@ -30,13 +30,11 @@ struct FeedOperand {
     bool padded;     // zeros follow each row's elements up to a multiple of 16 bytes
 };
 
-// An output array of rows x cols elements of `size` bytes; wide: 1 where every fourth column starts at a multiple of four elements' bytes, so that four leave in one
-// store, 2 where rows start at multiples of 16 bytes
+// An output array of elements of `size` bytes
 struct FeedOut {
     char* base;
     int64_t ld;      // bytes
     int32_t size;
-    int32_t wide;
 };
 
 // Which product: the contraction is contiguous in both operands and the columns come in pairs (gated), in both (plain), in the
@@ -62,7 +60,6 @@ struct FeedArgs {
     FeedOut gate_out;
     const char* grad_out;
     int64_t grad_out_ld;       // bytes
-    int32_t grad_out_wide;
     int32_t grad_cols;
 };
 
@@ -75,9 +72,19 @@ struct GateArgs {
     char *grad_gate, *grad_up;
     int64_t ld;                // bytes
     int64_t T, F, cols;        // cols: columns written, zeros from F on
-    int32_t activation, wide;  // wide: 16-byte loads
+    int32_t activation;
 };
 int launch_gate_grad(const GateArgs& a, int dtype, void* stream);
+
+// Rows of up to three arrays, `bytes` long, to rows of `ld` bytes one after another in `to`, zeros behind them
+struct PadArgs {
+    const char* from[3];
+    int64_t ld_from[3], rows[3];
+    char* to;
+    int64_t bytes, ld;         // ld: a multiple of 16
+    int32_t size;              // of an element
+};
+int launch_pad(const PadArgs& a, void* stream);
 
 struct QuantizeArgs {
     const char* x;
@@ -87,7 +94,6 @@ struct QuantizeArgs {
     float* scale;
     int64_t T, C;
     int32_t blocks;            // of 128 columns
-    int32_t wide;              // rows of x and q start at multiples of 16 and 8 bytes
 };
 int launch_quantize(const QuantizeArgs& a, int dtype, int block_rows, void* stream);
 

@@ -10,6 +10,13 @@ namespace cacnn {
 
 typedef unsigned int eu32x2 __attribute__((ext_vector_type(2)));
 typedef unsigned int eu32x4 __attribute__((ext_vector_type(4)));
+// 16 and 8 bytes at any address: the memory takes them in one access, over two lines where they lie so
+struct __attribute__((packed, aligned(1))) FeedBytes16 {
+    eu32x4 v;
+};
+struct __attribute__((packed, aligned(1))) FeedBytes8 {
+    eu32x2 v;
+};
 
 // ---- quantisation
 // A block's scale is the smallest power of two, from 2^-126 on, by which its largest finite magnitude a is at most 448, the largest number
@@ -33,12 +40,12 @@ struct Eight {
         if constexpr (DT == FEED_F32) return __uint_as_float(w[i]);
         else return __uint_as_float(i & 1 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16);
     }
-    // the first n of them, zeros behind; wide: 16-byte loads are possible
-    __device__ __forceinline__ void load(const char* p, int n, bool wide) {
-        if (wide && n >= 8) {
+    // the first n of them, zeros behind
+    __device__ __forceinline__ void load(const char* p, int n) {
+        if (n >= 8) {
 #pragma unroll
             for (int i = 0; i < (DT == FEED_F32 ? 2 : 1); ++i) {
-                const eu32x4 v = ((const eu32x4*)p)[i];
+                const eu32x4 v = ((const FeedBytes16*)p)[i].v;
 #pragma unroll
                 for (int e = 0; e < 4; ++e) w[i * 4 + e] = v[e];
             }
@@ -76,9 +83,9 @@ struct Eight {
     }
 };
 
-__device__ __forceinline__ void store_eight(uint8_t* p, int n, bool wide, eu32x2 q) {
-    if (wide && n >= 8) {
-        *(eu32x2*)p = q;
+__device__ __forceinline__ void store_eight(uint8_t* p, int n, eu32x2 q) {
+    if (n >= 8) {
+        ((FeedBytes8*)p)->v = q;
     } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i)
@@ -93,12 +100,12 @@ __global__ void __launch_bounds__(256) quantize_rows_kernel(const QuantizeArgs a
     const int n = (int)min((int64_t)8, a.C - col);
     for (int64_t t = blockIdx.y; t < a.T; t += gridDim.y) {
         Eight<DT> x;
-        x.load(a.x + t * a.ld_x + (int64_t)col * feed_size(DT), n, a.wide);
+        x.load(a.x + t * a.ld_x + (int64_t)col * feed_size(DT), n);
         uint32_t largest = x.largest();
 #pragma unroll
         for (int d = 1; d < 16; d *= 2) largest = max(largest, (uint32_t)__shfl_xor((int)largest, d));
         const int e = scale_power(largest);
-        if (n > 0) store_eight(a.q + t * a.ld_q + col, n, a.wide, x.quantized(e));
+        if (n > 0) store_eight(a.q + t * a.ld_q + col, n, x.quantized(e));
         if ((threadIdx.x & 15) == 0 && n > 0) a.scale[t * a.blocks + col / kScaleBlock] = power_of_two(e);
     }
 }
@@ -116,7 +123,7 @@ __global__ void __launch_bounds__(256) quantize_blocks_kernel(const QuantizeArgs
         uint32_t largest = 0;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            x[i].load(a.x + (t0 + i * 16) * a.ld_x + (int64_t)col * feed_size(DT), t0 + i * 16 < a.T ? n : 0, a.wide);
+            x[i].load(a.x + (t0 + i * 16) * a.ld_x + (int64_t)col * feed_size(DT), t0 + i * 16 < a.T ? n : 0);
             largest = max(largest, x[i].largest());
         }
 #pragma unroll
@@ -128,7 +135,7 @@ __global__ void __launch_bounds__(256) quantize_blocks_kernel(const QuantizeArgs
         if (threadIdx.x == 0) a.scale[b * a.blocks + blockIdx.x] = power_of_two(e);
 #pragma unroll
         for (int i = 0; i < 8; ++i)
-            if (t0 + i * 16 < a.T && n > 0) store_eight(a.q + (t0 + i * 16) * a.ld_q + col, n, a.wide, x[i].quantized(e));
+            if (t0 + i * 16 < a.T && n > 0) store_eight(a.q + (t0 + i * 16) * a.ld_q + col, n, x[i].quantized(e));
     }
 }
 
@@ -159,9 +166,9 @@ __global__ void __launch_bounds__(256) gate_grad_kernel(const GateArgs a) {
     if (t >= a.T) return;
     const int n = (int)max((int64_t)0, min((int64_t)8, a.F - col));
     Eight<DT> g, u, d;
-    g.load(a.gate + t * a.ld_pre + col * feed_size(DT), n, a.wide);
-    u.load(a.up + t * a.ld_pre + col * feed_size(DT), n, a.wide);
-    d.load(a.grad_out + t * a.ld_out + col * feed_size(DT), n, a.wide);
+    g.load(a.gate + t * a.ld_pre + col * feed_size(DT), n);
+    u.load(a.up + t * a.ld_pre + col * feed_size(DT), n);
+    d.load(a.grad_out + t * a.ld_out + col * feed_size(DT), n);
     uint32_t wg[8], wu[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
@@ -189,6 +196,42 @@ int launch_gate_grad(const GateArgs& a, int dtype, void* stream) {
     if (grid > INT32_MAX) return 1;
     if (dtype == FEED_F32) hipLaunchKernelGGL(gate_grad_kernel<FEED_F32>, dim3((uint32_t)grid), dim3(256), 0, (hipStream_t)stream, a);
     else hipLaunchKernelGGL(gate_grad_kernel<FEED_BF16>, dim3((uint32_t)grid), dim3(256), 0, (hipStream_t)stream, a);
+    return hipGetLastError() == hipSuccess ? 0 : 1;
+}
+
+// ---- arrays whose rows 16-byte loads cannot start with, to rows where they can: a piece of 16 bytes a thread
+__global__ void __launch_bounds__(256) pad_kernel(const PadArgs a) {
+    const uint32_t pieces = (uint32_t)(a.ld / 16);
+    const uint64_t first = (uint64_t)blockIdx.x * 256, row0 = first / pieces;
+    const uint32_t in = (uint32_t)(first - row0 * pieces) + threadIdx.x;
+    int64_t row = (int64_t)(row0 + in / pieces);
+    const int64_t at = (int64_t)(in % pieces) * 16;
+    char* const to = a.to + row * a.ld + at;
+    int i = 0;
+    while (i < 3 && row >= a.rows[i]) row -= a.rows[i++];
+    if (i == 3) return;
+    const char* const from = (i == 0 ? a.from[0] : i == 1 ? a.from[1] : a.from[2]) + row * (i == 0 ? a.ld_from[0] : i == 1 ? a.ld_from[1] : a.ld_from[2]) + at;
+    eu32x4 v = {0, 0, 0, 0};
+    if (at + 16 <= a.bytes) {
+        v = ((const FeedBytes16*)from)->v;
+    } else {
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            if (a.size == 4) {
+                if (at + w * 4 < a.bytes) v[w] = *(const uint32_t*)(from + w * 4);
+            } else {
+                if (at + w * 4 < a.bytes) v[w] = *(const uint16_t*)(from + w * 4);
+                if (at + w * 4 + 2 < a.bytes) v[w] |= (uint32_t)*(const uint16_t*)(from + w * 4 + 2) << 16;
+            }
+        }
+    }
+    *(eu32x4*)to = v;
+}
+
+int launch_pad(const PadArgs& a, void* stream) {
+    const int64_t grid = ((a.rows[0] + a.rows[1] + a.rows[2]) * (a.ld / 16) + 255) / 256;
+    if (grid > INT32_MAX) return 1;
+    if (grid > 0) hipLaunchKernelGGL(pad_kernel, dim3((uint32_t)grid), dim3(256), 0, (hipStream_t)stream, a);
     return hipGetLastError() == hipSuccess ? 0 : 1;
 }
 

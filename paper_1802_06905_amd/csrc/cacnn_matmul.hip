@@ -35,9 +35,12 @@ typedef short ms16x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 mbf16x8 __attribute__((ext_vector_type(8)));
 #define MAT_LDS(T) __attribute__((address_space(3))) T
 #define MAT_CONST(T) __attribute__((address_space(4))) const T
-// 16 bytes at any address
+// 16 and 8 bytes at any address: the memory takes them in one access, over two lines where they lie so
 struct __attribute__((packed, aligned(1))) MatBytes16 {
     mu32x4 v;
+};
+struct __attribute__((packed, aligned(1))) MatBytes8 {
+    mu32x2 v;
 };
 
 // Where the strided operand's block b of contraction index k lies: b ^ strided_turn.  The lanes of one access have k = 8 g + (0..3) (bf16, blocks of
@@ -319,10 +322,10 @@ __device__ __forceinline__ void store_run(const FeedOut& o, int64_t m, int64_t n
     constexpr bool WORDS = DT == FEED_F32 || DT == FEED_E4M3_EXACT;
     static_assert(E == 4 || (E == 8 && !WORDS), "what one store takes");
     char* const p = o.base + m * o.ld + n * (WORDS ? 4 : 2);
-    if ((E * (WORDS ? 4 : 2) == 16 ? o.wide == 2 : o.wide != 0) && n + E <= cols) {
-        if constexpr (WORDS) *(mf32x4*)p = mf32x4{v[0], v[1], v[2], v[3]};
-        else if constexpr (E == 4) *(mu32x2*)p = mu32x2{two_bf16(v[0], v[1]), two_bf16(v[2], v[3])};
-        else *(mu32x4*)p = mu32x4{two_bf16(v[0], v[1]), two_bf16(v[2], v[3]), two_bf16(v[4], v[5]), two_bf16(v[6], v[7])};
+    if (n + E <= cols) {
+        if constexpr (WORDS) ((MatBytes16*)p)->v = __builtin_bit_cast(mu32x4, mf32x4{v[0], v[1], v[2], v[3]});
+        else if constexpr (E == 4) ((MatBytes8*)p)->v = mu32x2{two_bf16(v[0], v[1]), two_bf16(v[2], v[3])};
+        else ((MatBytes16*)p)->v = mu32x4{two_bf16(v[0], v[1]), two_bf16(v[2], v[3]), two_bf16(v[4], v[5]), two_bf16(v[6], v[7])};
     } else {
 #pragma unroll
         for (int e = 0; e < E; ++e)
@@ -343,15 +346,15 @@ __device__ __forceinline__ void finish_run(const FeedArgs& a, int product, int64
         if (n >= a.grad_cols) return;
         float d[E];
         const char* const p = a.grad_out + m * a.grad_out_ld + n * feed_size(DT);
-        if (a.grad_out_wide && n + E <= a.N) {
+        if (n + E <= a.N) {
 #pragma unroll
             for (int e = 0; e < E; e += 4) {
                 if constexpr (DT == FEED_F32) {
-                    const mf32x4 w = *(const mf32x4*)(p + e * 4);
+                    const mf32x4 w = __builtin_bit_cast(mf32x4, ((const MatBytes16*)(p + e * 4))->v);
 #pragma unroll
                     for (int x = 0; x < 4; ++x) d[e + x] = w[x];
                 } else {
-                    const mu32x2 w = *(const mu32x2*)(p + e * 2);
+                    const mu32x2 w = ((const MatBytes8*)(p + e * 2))->v;
 #pragma unroll
                     for (int x = 0; x < 4; ++x) d[e + x] = __uint_as_float(x & 1 ? w[x / 2] & 0xffff0000u : w[x / 2] << 16);
                 }

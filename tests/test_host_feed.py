@@ -79,6 +79,9 @@ def test_workspace():
     assert cc.cacnn_gated_workspace((4, 256, 64, 0), 1) == 2 * 4 * 64 * 2
     assert cc.cacnn_gated_workspace((5, 256, 65, 0), 0) == 2 * 5 * 128 * 4
     assert cc.cacnn_gated_workspace((1 << 20, 8, 1 << 16, 2), 1) == 2 << 37
+    # rows of C elements that are no multiple of 16 bytes are copied where there are enough of them
+    assert cc.cacnn_gated_workspace((500, 7, 65, 0), 0) == 2 * 500 * 128 * 4 + (500 + 2 * 65) * 64 * 4
+    assert cc.cacnn_gated_workspace((500, 8, 65, 0), 0) == cc.cacnn_gated_workspace((500, 12, 65, 0), 0) == 2 * 500 * 128 * 4
     for bad, status in (((4, 0, 64, 0), INVALID), ((4, 8, 64, 7), UNSUPPORTED)):
         with pytest.raises(cc.CacnnError) as e:
             cc.cacnn_gated_workspace(bad, 1)
