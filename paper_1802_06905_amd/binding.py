@@ -302,7 +302,8 @@ def _native_interface():
     """What the module is told of the library: the interface it must have been compiled for, and where its calls are."""
     address = lambda f: ctypes.cast(f, ctypes.c_void_p).value  # noqa: E731
     return (_lib.cacnn_internal_sized_interface(), ctypes.sizeof(Problem), Problem,
-            address(_lib.cacnn_internal_conv_forward_sized), address(_lib.cacnn_internal_pool_forward_sized))
+            address(_lib.cacnn_internal_conv_forward_sized), address(_lib.cacnn_internal_pool_forward_sized), address(_lib.cacnn_quantize),
+            address(_lib.cacnn_matmul_scaled), address(_lib.cacnn_gated_forward), address(_lib.cacnn_gated_forward_scaled))
 
 
 def _load_native():
@@ -509,6 +510,16 @@ def _feed_dtype(where: str, dtype):
     return (_FEED_DTYPE[int(dtype)],)
 
 
+def _feed_native(where: str, *args) -> bool:
+    """Whether the module took the call (as in cacnn_conv_forward; what it does not take, or finds fault with, goes the way that says what is wrong)."""
+    if _native is None or not (args[-1] is None or type(args[-1]) is int):
+        return False
+    rc = getattr(_native, where[6:])(*args)
+    if rc > 0 and rc not in _ARGUMENT_ERRORS:
+        raise CacnnError(rc, where)
+    return rc == 0
+
+
 class _Feed:
     """Checks of one call: every tensor's type, shape and layout against the problem, all on the device of `stream` (which is the current one
     of the tensors' device where none is given).  The library trusts its pointers."""
@@ -565,6 +576,8 @@ class _Feed:
 def cacnn_quantize(problem, dtype: int, x, q, scale, stream=None) -> None:
     """Enqueue the quantisation of X[T,C] to 8-bit floats Q[T,C] with a scale for each block of 128 columns and problem.block_rows (1 or 128)
     rows, scale[ceil(T/block_rows), ceil(C/128)] fp32.  problem: QuantizeProblem or (T, C, block_rows)."""
+    if _feed_native("cacnn_quantize", problem, dtype, x, q, scale, stream):
+        return
     f = _Feed("cacnn_quantize", problem, QuantizeProblem, stream)
     p = f.problem
     if p.block_rows not in (1, 128):
@@ -576,6 +589,8 @@ def cacnn_quantize(problem, dtype: int, x, q, scale, stream=None) -> None:
 def cacnn_matmul_scaled(problem, x, x_scale, w, w_scale, out_dtype: int, out, stream=None) -> None:
     """Enqueue Out[T,K] = X[T,C] W[K,C]' of 8-bit floats (torch.float8_e4m3fn, or their bytes) with scales x_scale[T, ceil(C/128)] and
     w_scale[ceil(K/128), ceil(C/128)].  problem: MatmulProblem or (T, C, K)."""
+    if _feed_native("cacnn_matmul_scaled", problem, x, x_scale, w, w_scale, out_dtype, out, stream):
+        return
     f = _Feed("cacnn_matmul_scaled", problem, MatmulProblem, stream)
     p = f.problem
     blocks = -(-p.C // 128)
@@ -587,6 +602,8 @@ def cacnn_matmul_scaled(problem, x, x_scale, w, w_scale, out_dtype: int, out, st
 def cacnn_gated_forward(problem, dtype: int, x, w_gate, w_up, out, gate=None, up=None, stream=None) -> None:
     """Enqueue Out[T,F] = act(X[T,C] W_gate[F,C]') * (X W_up[F,C]'), and, where tensors are given for them, the two products gate[T,F]
     and up[T,F].  problem: GatedProblem or (T, C, F, activation)."""
+    if _feed_native("cacnn_gated_forward", problem, dtype, x, w_gate, w_up, out, gate, up, stream):
+        return
     f = _Feed("cacnn_gated_forward", problem, GatedProblem, stream)
     p, t = f.problem, _feed_dtype("cacnn_gated_forward", dtype)
     f.call(_lib.cacnn_gated_forward, int(dtype), f.take("x", x, p.T, p.C, t, "ld_x"), f.take("w_gate", w_gate, p.F, p.C, t, "ld_w"),
@@ -596,6 +613,8 @@ def cacnn_gated_forward(problem, dtype: int, x, w_gate, w_up, out, gate=None, up
 
 def cacnn_gated_forward_scaled(problem, x, x_scale, w_gate, w_gate_scale, w_up, w_up_scale, out_dtype: int, out, stream=None) -> None:
     """cacnn_gated_forward of 8-bit floats with scales as for cacnn_matmul_scaled; Out in out_dtype."""
+    if _feed_native("cacnn_gated_forward_scaled", problem, x, x_scale, w_gate, w_gate_scale, w_up, w_up_scale, out_dtype, out, stream):
+        return
     f = _Feed("cacnn_gated_forward_scaled", problem, GatedProblem, stream)
     p = f.problem
     blocks, fp32 = -(-p.C // 128), (torch.float32,)

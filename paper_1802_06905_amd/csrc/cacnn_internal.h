@@ -10,9 +10,10 @@
 
 namespace cacnn {
 
-// What cacnn_torch.cpp takes on trust of the library: the problem's layout and the signatures of cacnn_internal_conv_forward_sized and
-// cacnn_internal_pool_forward_sized.  To be raised with any of them; a module and a library that differ are not used together.
-constexpr int kSizedInterface = 1;
+// What cacnn_torch.cpp takes on trust of the library: the problems' layouts and the signatures of cacnn_internal_conv_forward_sized,
+// cacnn_internal_pool_forward_sized, cacnn_quantize, cacnn_matmul_scaled and the two forward calls of the gated projection.  To be raised with any of
+// them; a module and a library that differ are not used together.
+constexpr int kSizedInterface = 2;
 
 // Set-up that a process needs once for each device: done(device, set_up) calls set_up() until it has succeeded there.  A failure is not
 // remembered; threads that come at the same time may both set up.
