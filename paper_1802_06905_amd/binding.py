@@ -303,7 +303,8 @@ def _native_interface():
     address = lambda f: ctypes.cast(f, ctypes.c_void_p).value  # noqa: E731
     return (_lib.cacnn_internal_sized_interface(), ctypes.sizeof(Problem), Problem,
             address(_lib.cacnn_internal_conv_forward_sized), address(_lib.cacnn_internal_pool_forward_sized), address(_lib.cacnn_quantize),
-            address(_lib.cacnn_matmul_scaled), address(_lib.cacnn_gated_forward), address(_lib.cacnn_gated_forward_scaled))
+            address(_lib.cacnn_matmul_scaled), address(_lib.cacnn_gated_forward), address(_lib.cacnn_gated_forward_scaled),
+            address(_lib.cacnn_gated_backward))
 
 
 def _load_native():
@@ -639,6 +640,8 @@ def cacnn_gated_backward(problem, dtype: int, x, w_gate, w_up, grad_out, grad_x,
     """Enqueue the gradients of cacnn_gated_forward for grad_out[T,F]: grad_x[T,C] and grad_w_gate, grad_w_up[F,C] (None: not wanted).  gate and up
     are what the forward pass kept, or None.  workspace: a contiguous tensor of at least cacnn_gated_workspace bytes, one for each call
     that may run at the same time."""
+    if _feed_native("cacnn_gated_backward", problem, dtype, x, w_gate, w_up, grad_out, grad_x, grad_w_gate, grad_w_up, workspace, gate, up, stream):
+        return
     f = _Feed("cacnn_gated_backward", problem, GatedProblem, stream)
     p, t = f.problem, _feed_dtype("cacnn_gated_backward", dtype)
 

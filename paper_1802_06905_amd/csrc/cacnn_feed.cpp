@@ -3,6 +3,7 @@
 
 #include <algorithm>
 #include <climits>
+#include <cmath>
 
 #include "../../include/cacnn.h"
 #include "cacnn_feed.h"
@@ -56,7 +57,49 @@ int launched(int rc) { return rc == 0 ? CACNN_OK : CACNN_ERR_LAUNCH; }
 
 }  // namespace
 
+// The kernel with the least estimated time.  A workgroup has a compute unit to itself (two of the 128 x 128 tiles with two stages share one), a launch runs in
+// rounds of 256, and a round takes 3 us and what a slab of 128 bytes of the contraction (the dividing waves: four slabs, one each) was measured to take, in us, on
+// shapes of 64 to 8192 rows; operands that come through registers take the dividing waves, which are then one slab ahead only, twice as long:
+//                                            bf16, 8 bits   fp32 (bound by its matrix instructions)
+//     32 x 32 divided (gated: 32 x 2 x 32)   0.75 (1.15)     0.8 (1.15)
+//     64 x 32 divided (gated: 64 x 2 x 32)   1.15 (1.25)     1.2 (1.9)
+//     64 x 64 divided                        1.45            1.9
+//     128 x 128, four stages                 0.85            2.0
+//     128 x 128, two of two stages           1.6             3.8
+//     256 x 256                              2.0             -
+// Examples, us, the chosen kernel first: 8 bits (64, 8192, 4096) 15 on 32 x 32, 22 on 64 x 32; (256, 4096, 4096) 15.5 on 64 x 64, 22 on 64 x 32; (1024, 4096, 4096)
+// 34 on 128 x 128 with four stages, 39 with two, 47 on 64 x 64; (2048, 4096, 4096) 51 with two stages, 64 with four, 78 on 256 x 256; bf16 gated (8192, 4096, 8192)
+// 972 on 256 x 256, 1135 on 128 x 128 with two stages.
+int cacnn::matmul_kernel(const FeedArgs& a, int form, int dtype, bool direct) {
+    const bool f32 = dtype == FEED_F32, gated = form == FEED_GATED;
+    const int64_t half = gated ? 2 : 1;
+    const double slabs = (double)a.q[0].k * feed_size(dtype) / 128 * a.segments, ahead = direct ? 1.0 : 2.0;
+    auto us = [&](int64_t rows, int64_t cols, int waves, double slab_us, int64_t at_once = 256) {
+        const int64_t tiles = (a.M + rows - 1) / rows * ((a.N + cols - 1) / cols) * a.products;
+        return (double)((tiles + at_once - 1) / at_once) * (3.0 + std::ceil(slabs / waves) * slab_us);
+    };
+    int best = MATMUL_WAVES_32;
+    double least = us(32, 32, 4, ahead * (gated ? 1.15 : f32 ? 0.8 : 0.75));
+    auto candidate = [&](int kernel, double t) {
+        if (t < least) least = t, best = kernel;
+    };
+    candidate(MATMUL_WAVES_64_32, us(64, 32, 4, ahead * (gated ? (f32 ? 1.9 : 1.25) : f32 ? 1.2 : 1.15)));
+    if (!gated) candidate(MATMUL_WAVES_64, us(64, 64, 4, ahead * (f32 ? 1.9 : 1.45)));
+    if (direct) candidate(MATMUL_128_DEEP, us(128, 128 / half, 1, f32 ? 2.0 : 0.85));
+    candidate(MATMUL_128, us(128, 128 / half, 1, f32 ? 3.8 : 1.6, 512));
+    if (direct && (dtype == FEED_BF16 || dtype == FEED_E4M3)) candidate(MATMUL_256, us(256, 256 / half, 1, 2.0));
+    return best;
+}
+
 extern "C" {
+
+// The kernel (its number in cacnn_feed.h) of a product with M x N results and a contraction of k elements: form and dtype as there
+int cacnn_internal_matmul_kernel(int form, int dtype, int direct, int64_t M, int64_t N, int64_t k) {
+    FeedArgs a = {};
+    a.M = M, a.N = N, a.q[0].k = k;
+    a.segments = form == FEED_RIGHT ? 2 : 1, a.products = form == FEED_BOTH ? 2 : 1;
+    return matmul_kernel(a, form, dtype, direct != 0);
+}
 
 int cacnn_quantize(const cacnn_quantize_problem* problem, int dtype, const void* x, void* q, float* scale, void* hip_stream) {
     if (!problem || (problem->T != 0 && (!x || !q || !scale))) return CACNN_ERR_NULL;

@@ -63,6 +63,12 @@ struct FeedArgs {
     int32_t grad_cols;
 };
 
+// The kernels of a product: workgroups whose four waves divide the contraction, with 32 x 32, 64 x 32 and 64 x 64 of the sums (gated: half as many columns of
+// Out), and workgroups with 128 x 128 (four stages in LDS, or two and two workgroups to a compute unit) and 256 x 256
+enum { MATMUL_WAVES_32 = 0, MATMUL_WAVES_64_32 = 1, MATMUL_WAVES_64 = 2, MATMUL_128_DEEP = 3, MATMUL_128 = 4, MATMUL_256 = 5 };
+// Which of them takes the product of operands that go straight to LDS or (direct false) through registers
+int matmul_kernel(const FeedArgs& a, int form, int dtype, bool direct);
+
 // Launches the product; form, dtype as above.  0, or 1 where the runtime refused.
 int launch_matmul(const FeedArgs& a, int form, int dtype, void* stream);
 

@@ -11,9 +11,9 @@
 namespace cacnn {
 
 // What cacnn_torch.cpp takes on trust of the library: the problems' layouts and the signatures of cacnn_internal_conv_forward_sized,
-// cacnn_internal_pool_forward_sized, cacnn_quantize, cacnn_matmul_scaled and the two forward calls of the gated projection.  To be raised with any of
+// cacnn_internal_pool_forward_sized, cacnn_quantize, cacnn_matmul_scaled and the gated projection's three.  To be raised with any of
 // them; a module and a library that differ are not used together.
-constexpr int kSizedInterface = 2;
+constexpr int kSizedInterface = 3;
 
 // Set-up that a process needs once for each device: done(device, set_up) calls set_up() until it has succeeded there.  A failure is not
 // remembered; threads that come at the same time may both set up.

@@ -15,8 +15,6 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
-#include <cmath>
-
 #include "cacnn_feed.h"
 #include "cacnn_gate.h"
 #include "cacnn_internal.h"
@@ -892,53 +890,21 @@ static int launch_waves(const FeedArgs& a, void* stream) {
 static bool direct(const FeedOperand& o, int size, bool strided) {
     return reinterpret_cast<uintptr_t>(o.base) % 16 == 0 && o.ld % 16 == 0 && (o.padded || (strided ? o.rows : o.k) * size % 16 == 0);
 }
-// Which kernel: the one with the least estimated time.  A workgroup of 256 or 512 threads has a compute unit to itself (two of the 128 x 128 tiles with two
-// stages share one), a launch runs in rounds of 256, and a round takes 3 us and what a slab of 128 bytes (the dividing waves: four slabs, one each) was
-// measured to take, in us, on shapes of 64 to 8192 rows:
-//                                   bf16, 8 bits    fp32 (bound by its matrix instructions)
-//     32 x 32 divided (gated: 32 x 2 x 32)   0.75 (1.15)     0.8 (1.2)
-//     64 x 32 divided (gated: 64 x 2 x 32)   1.15 (1.25)     1.2 (1.9)
-//     64 x 64 divided                        1.45            1.9
-//     128 x 128, four stages                 0.85            1.9
-//     128 x 128, two of two stages           1.6             3.8
-//     256 x 256                              2.0             -
-// Examples, us, the chosen kernel first: 8 bits (64, 8192, 4096) 15 on 32 x 32, 22 on 64 x 32; (256, 4096, 4096) 15.5 on 64 x 64, 22 on 64 x 32; (1024, 4096, 4096)
-// 34 on 128 x 128 with four stages, 39 with two, 47 on 64 x 64; (2048, 4096, 4096) 51 with two stages, 64 with four, 78 on 256 x 256.
-struct Estimate {
-    double slabs;        // of 128 bytes
-    const FeedArgs* a;
-    double us(int64_t rows, int64_t cols, int waves, double slab_us, int per_unit = 1) const {
-        const int64_t t = (a->M + rows - 1) / rows * ((a->N + cols - 1) / cols) * a->products, at_once = 256 * per_unit;
-        return (double)((t + at_once - 1) / at_once) * (3.0 + std::ceil(slabs / waves) * slab_us);
-    }
-};
-
 template <int DT, int FORM, bool QD, bool PD>
 static int launch_shape(const FeedArgs& a, void* stream) {
-    constexpr bool F32 = DT == FEED_F32, GATED = FORM == FEED_GATED, DIRECT = QD && PD;
-    constexpr int HALF = GATED ? 2 : 1;
-    const Estimate e = {(double)a.q[0].k * feed_size(DT) / 128 * a.segments, &a};
-    constexpr double AHEAD = DIRECT ? 1.0 : 2.0;         // (through registers a dividing wave is one slab ahead)
-    double least = e.us(32, 32, 4, AHEAD * (GATED ? 1.15 : F32 ? 0.8 : 0.75));
-    int best = 0;
-    auto candidate = [&](int kernel, double us) {
-        if (us < least) least = us, best = kernel;
-    };
-    candidate(1, e.us(64, 32, 4, AHEAD * (GATED ? (F32 ? 1.9 : 1.25) : F32 ? 1.2 : 1.15)));
-    if constexpr (!GATED) candidate(2, e.us(64, 64, 4, AHEAD * (F32 ? 1.9 : 1.45)));
-    if constexpr (DIRECT) candidate(3, e.us(128, 128 / HALF, 1, F32 ? 1.9 : 0.85));
-    candidate(4, e.us(128, 128 / HALF, 1, F32 ? 3.8 : 1.6, 2));
-    if constexpr (DIRECT && (DT == FEED_BF16 || DT == FEED_E4M3)) candidate(5, e.us(256, 256 / HALF, 1, 2.0));
-    if (best == 0) return launch_waves<DT, FORM, 1, HALF, QD, PD>(a, stream);
-    if (best == 1) return launch_waves<DT, FORM, 2, HALF, QD, PD>(a, stream);
-    if constexpr (!GATED)
-        if (best == 2) return launch_waves<DT, FORM, 2, 2, QD, PD>(a, stream);
+    constexpr bool DIRECT = QD && PD;
+    constexpr int HALF = FORM == FEED_GATED ? 2 : 1;
+    const int kernel = matmul_kernel(a, FORM, DT, DIRECT);
+    if (kernel == MATMUL_WAVES_32) return launch_waves<DT, FORM, 1, HALF, QD, PD>(a, stream);
+    if (kernel == MATMUL_WAVES_64_32) return launch_waves<DT, FORM, 2, HALF, QD, PD>(a, stream);
+    if constexpr (FORM != FEED_GATED)
+        if (kernel == MATMUL_WAVES_64) return launch_waves<DT, FORM, 2, 2, QD, PD>(a, stream);
     if constexpr (DIRECT)
-        if (best == 3) return launch_block<DT, FORM, 2, 2, 2, 2, 128, 4, QD, PD>(a, stream);
+        if (kernel == MATMUL_128_DEEP) return launch_block<DT, FORM, 2, 2, 2, 2, 128, 4, QD, PD>(a, stream);
     if constexpr (DIRECT && DT == FEED_BF16)
-        if (best == 5) return launch_block<DT, FORM, 4, 2, 2, 4, 64, 4, QD, PD>(a, stream);
+        if (kernel == MATMUL_256) return launch_block<DT, FORM, 4, 2, 2, 4, 64, 4, QD, PD>(a, stream);
     if constexpr (DIRECT && DT == FEED_E4M3)
-        if (best == 5) return launch_block<DT, FORM, 4, 2, 2, 4, 128, 2, QD, PD>(a, stream);
+        if (kernel == MATMUL_256) return launch_block<DT, FORM, 4, 2, 2, 4, 128, 2, QD, PD>(a, stream);
     return launch_block<DT, FORM, 2, 2, 2, 2, 128, 2, QD, PD>(a, stream);
 }
 template <int DT, int FORM>

@@ -21,6 +21,7 @@ using QuantizeFn = decltype(&cacnn_quantize);
 using MatmulFn = decltype(&cacnn_matmul_scaled);
 using GatedFn = decltype(&cacnn_gated_forward);
 using GatedScaledFn = decltype(&cacnn_gated_forward_scaled);
+using GatedBackwardFn = decltype(&cacnn_gated_backward);
 
 constexpr Py_ssize_t kProblemBytes = 9 * 8;
 PyTypeObject* g_problem = nullptr;   // the binding's Problem, a ctypes structure
@@ -30,6 +31,7 @@ QuantizeFn g_quantize = nullptr;
 MatmulFn g_matmul = nullptr;
 GatedFn g_gated = nullptr;
 GatedScaledFn g_gated_scaled = nullptr;
+GatedBackwardFn g_gated_backward = nullptr;
 
 PyObject* not_tried() { return PyLong_FromLong(-1); }
 
@@ -258,19 +260,51 @@ PyObject* gated_forward_scaled(PyObject*, PyObject* const* args, Py_ssize_t n) {
     END_HANDLE_TH_ERRORS
 }
 
+// gated_backward(problem, dtype, x, w_gate, w_up, grad_out, grad_x, grad_w_gate, grad_w_up, workspace, gate, up, stream)
+PyObject* gated_backward(PyObject*, PyObject* const* args, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    if (n != 13 || !g_gated_backward) return not_tried();
+    Feed f(args[0], 4);
+    int dtype = 0;
+    at::ScalarType type;
+    void* stream = nullptr;
+    if (!f.type_of(args[1], &dtype, &type)) return not_tried();
+    cacnn_gated_problem p = {f.size[0], f.size[1], f.size[2], f.size[3], 0, 0, 0, 0, 0, 0};
+    const void* const x = f.take(args[2], type, p.T, p.C, &p.ld_x);
+    const void* const wg = f.take(args[3], type, p.F, p.C, &p.ld_w);
+    const void* const wu = f.take(args[4], type, p.F, p.C, &p.ld_w);
+    const void* const grad_out = f.take(args[5], type, p.T, p.F, &p.ld_out);
+    void* const grad_x = f.take_or_none(args[6], type, p.T, p.C, &p.ld_grad_x);
+    void* const grad_wg = f.take_or_none(args[7], type, p.F, p.C, &p.ld_grad_w);
+    void* const grad_wu = f.take_or_none(args[8], type, p.F, p.C, &p.ld_grad_w);
+    const void* const gate = f.take_or_none(args[10], type, p.T, p.F, &p.ld_pre);
+    const void* const up = f.take_or_none(args[11], type, p.T, p.F, &p.ld_pre);
+    if (!f.usual || !THPVariable_CheckExact(args[9]) || !stream_of(args[12], &stream)) return not_tried();
+    const at::Tensor& work = THPVariable_Unpack(args[9]);
+    if (!work.is_cuda() || work.get_device() != f.device || !work.is_contiguous()) return not_tried();
+    void* const workspace = work.data_ptr();
+    const size_t bytes = (size_t)work.numel() * work.element_size();
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = g_gated_backward(&p, dtype, x, wg, wu, gate, up, grad_out, grad_x, grad_wg, grad_wu, workspace, bytes, stream);
+    Py_END_ALLOW_THREADS
+    return PyLong_FromLong(rc);
+    END_HANDLE_TH_ERRORS
+}
+
 // setup(cacnn_internal_sized_interface(), size of Problem, Problem, addresses of cacnn_internal_conv_forward_sized,
-// cacnn_internal_pool_forward_sized, cacnn_quantize, cacnn_matmul_scaled, cacnn_gated_forward, cacnn_gated_forward_scaled); ImportError where the first two are not what this module was compiled for
+// cacnn_internal_pool_forward_sized, cacnn_quantize, cacnn_matmul_scaled, cacnn_gated_forward, cacnn_gated_forward_scaled, cacnn_gated_backward); ImportError where the first two are not what this module was compiled for
 PyObject* setup(PyObject*, PyObject* args) {
-    PyObject *problem, *at[6];
+    PyObject *problem, *at[7];
     int interface = 0;
     Py_ssize_t size = 0;
-    if (!PyArg_ParseTuple(args, "inO!OOOOOO", &interface, &size, &PyType_Type, &problem, &at[0], &at[1], &at[2], &at[3], &at[4], &at[5])) return nullptr;
+    if (!PyArg_ParseTuple(args, "inO!OOOOOOO", &interface, &size, &PyType_Type, &problem, &at[0], &at[1], &at[2], &at[3], &at[4], &at[5], &at[6])) return nullptr;
     if (interface != cacnn::kSizedInterface || size != kProblemBytes) {
         PyErr_SetString(PyExc_ImportError, "_cacnn_torch was compiled for another version of the library");
         return nullptr;
     }
-    void* f[6];
-    for (int i = 0; i < 6; ++i) f[i] = PyLong_AsVoidPtr(at[i]);
+    void* f[7];
+    for (int i = 0; i < 7; ++i) f[i] = PyLong_AsVoidPtr(at[i]);
     if (PyErr_Occurred()) return nullptr;
     Py_INCREF(problem);
     Py_XDECREF((PyObject*)g_problem);
@@ -281,6 +315,7 @@ PyObject* setup(PyObject*, PyObject* args) {
     g_matmul = (MatmulFn)f[3];
     g_gated = (GatedFn)f[4];
     g_gated_scaled = (GatedScaledFn)f[5];
+    g_gated_backward = (GatedBackwardFn)f[6];
     Py_RETURN_NONE;
 }
 
@@ -291,6 +326,7 @@ PyMethodDef g_methods[] = {
     {"matmul_scaled", (PyCFunction)(void (*)(void))matmul_scaled, METH_FASTCALL, nullptr},
     {"gated_forward", (PyCFunction)(void (*)(void))gated_forward, METH_FASTCALL, nullptr},
     {"gated_forward_scaled", (PyCFunction)(void (*)(void))gated_forward_scaled, METH_FASTCALL, nullptr},
+    {"gated_backward", (PyCFunction)(void (*)(void))gated_backward, METH_FASTCALL, nullptr},
     {"setup", setup, METH_VARARGS, nullptr},
     {nullptr, nullptr, 0, nullptr},
 };

@@ -177,3 +177,37 @@ def test_more_that_does_not_fit(calls):
     with pytest.raises(ValueError, match="workspace"):
         cc.cacnn_gated_backward((4, 256, 64, 0), 1, **grads, workspace=on(64, 64, dtype=torch.uint8).t())
     assert not calls
+
+
+# ---- which kernel a product runs on
+W32, W64_32, W64, DEEP, MIDDLE, LARGE = range(6)
+
+
+def kernel(form, dtype, M, N, k, direct=1):
+    LIB.cacnn_internal_matmul_kernel.argtypes = [ctypes.c_int] * 3 + [ctypes.c_int64] * 3
+    return LIB.cacnn_internal_matmul_kernel(form, dtype, direct, M, N, k)
+
+
+def test_a_kernel_for_every_size():
+    """Few rows are divided among waves, many rows take the large tiles, and nothing asks for a kernel that the type or its operands have not."""
+    plain, e4m3 = 1, 2
+    assert [kernel(plain, e4m3, T, 4096, 4096) for T in (1, 32, 256, 1024, 2048, 8192)] == [W32, W32, W64, DEEP, MIDDLE, LARGE]
+    assert [kernel(0, 1, T, 8192, 4096) for T in (1, 64, 256, 8192)] == [W32, W64_32, DEEP, LARGE]
+    for form in range(4):
+        for dtype in range(4):
+            for M in (1, 7, 100, 1000, 10000, (1 << 31) - 1):
+                for N in (1, 100, 5000, 1 << 20):
+                    for k in (0, 1, 100, 10000):
+                        assert kernel(form, dtype, M, N, k, 0) in ((W32, W64_32, MIDDLE) if form == 0 else (W32, W64_32, W64, MIDDLE))
+                        chosen = kernel(form, dtype, M, N, k)
+                        assert chosen != LARGE or dtype in (1, 2)
+                        assert form != 0 or chosen != W64
+
+
+def test_the_module_leaves_what_is_not_usual():
+    if binding._native is None:
+        pytest.skip("the module was not built")
+    t = torch.zeros((4, 256), dtype=torch.bfloat16)
+    for args in ((), (1,) * 6, ((4, 256, 1), 1, t, t, t, None), ((4, 256), 1, t, t, t, None), (cc.QuantizeProblem(4, 256, 1), 1, t, t, t, None),
+                 ((0, 256, 1), 1, t, t, t, None), ((4, 256, 1), 7, t, t, t, None), ((4, 256, 3), 1, t, t, t, None), ((1 << 40, 256, 1), 1, t, t, t, None)):
+        assert binding._native.quantize(*args) == -1
