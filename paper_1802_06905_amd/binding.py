@@ -652,7 +652,7 @@ def cacnn_gated_backward(problem, dtype: int, x, w_gate, w_up, grad_out, grad_x,
             optional("gate", gate, p.T, p.F, "ld_pre"), optional("up", up, p.T, p.F, "ld_pre"), f.take("grad_out", grad_out, p.T, p.F, t, "ld_out"),
             optional("grad_x", grad_x, p.T, p.C, "ld_grad_x"), optional("grad_w_gate", grad_w_gate, p.F, p.C, "ld_grad_w"),
             optional("grad_w_up", grad_w_up, p.F, p.C, "ld_grad_w")]
-    if workspace.device != f.device or not workspace.is_contiguous():
+    if not isinstance(workspace, torch.Tensor) or workspace.device != f.device or not workspace.is_contiguous():
         raise ValueError(f"{f.where}: workspace must be a contiguous tensor on {f.device}")
     f.call(_lib.cacnn_gated_backward, int(dtype), *args, workspace.data_ptr(), workspace.numel() * workspace.element_size())
 

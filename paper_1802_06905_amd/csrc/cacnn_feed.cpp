@@ -15,8 +15,8 @@ namespace {
 
 // Row lengths and strides: 32-bit offsets within the 256 rows of a tile, in units of a byte, stay below 2^30
 constexpr int64_t kMostColumns = 1 << 20, kMostRows = INT32_MAX;
-// and the workgroups of a launch are at most 2^31 - 1; a tile has at least 32 rows or columns
-bool tiles_in_range(int64_t rows, int64_t cols) { return (rows + 31) / 32 * ((cols + 31) / 32) <= INT32_MAX; }
+// and the threads of a launch below 2^32: 256 for each 128 x 64 of a gated projection's result
+bool tiles_in_range(int64_t rows, int64_t cols) { return (rows + 127) / 128 * ((cols + 63) / 64) < (1 << 24); }
 
 bool columns(int64_t n) { return n >= 1 && n <= kMostColumns; }
 bool rows(int64_t n) { return n >= 0 && n <= kMostRows; }
@@ -49,7 +49,7 @@ struct Workspace {
 bool valid_gated(cacnn_gated_problem* p) {
     return rows(p->T) && columns(p->C) && columns(p->F) && stride(&p->ld_x, p->C) && stride(&p->ld_w, p->C) && stride(&p->ld_out, p->F) &&
            stride(&p->ld_pre, p->F) && stride(&p->ld_grad_x, p->C) && stride(&p->ld_grad_w, p->C) && tiles_in_range(p->T, padded(p->F)) &&
-           tiles_in_range(p->T, p->C);
+           tiles_in_range(p->T, p->C) && tiles_in_range(2 * p->F, p->C);
 }
 bool activation(int64_t a) { return a == CACNN_GATE_SILU || a == CACNN_GATE_GELU || a == CACNN_GATE_GELU_TANH; }
 

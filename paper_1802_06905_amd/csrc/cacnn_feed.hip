@@ -156,14 +156,7 @@ int launch_quantize(const QuantizeArgs& a, int dtype, int block_rows, void* stre
 // ---- gradients of gate and up from the values that the forward pass kept, eight columns a thread; columns from F to `cols`, the end of a row in the
 // workspace, are written with zeros
 template <int DT>
-__global__ void __launch_bounds__(256) gate_grad_kernel(const GateArgs a) {
-    const uint32_t pieces = (uint32_t)(a.cols / 8);
-    const uint64_t first = (uint64_t)blockIdx.x * 256;
-    const uint64_t row0 = first / pieces;
-    const uint32_t in = (uint32_t)(first - row0 * pieces) + threadIdx.x;
-    const int64_t t = (int64_t)(row0 + in / pieces);
-    const int64_t col = (int64_t)(in % pieces) * 8;
-    if (t >= a.T) return;
+__device__ __forceinline__ void gate_grad_piece(const GateArgs& a, int64_t t, int64_t col) {
     const int n = (int)max((int64_t)0, min((int64_t)8, a.F - col));
     Eight<DT> g, u, d;
     g.load(a.gate + t * a.ld_pre + col * feed_size(DT), n);
@@ -191,25 +184,34 @@ __global__ void __launch_bounds__(256) gate_grad_kernel(const GateArgs a) {
     }
 }
 
+template <int DT>
+__global__ void __launch_bounds__(256) gate_grad_kernel(const GateArgs a) {
+    const uint32_t pieces = (uint32_t)(a.cols / 8);
+    // (the 64-bit division is uniform; a thread's own is of 32 bits)
+    for (uint64_t first = (uint64_t)blockIdx.x * 256; first < (uint64_t)a.T * pieces; first += (uint64_t)gridDim.x * 256) {
+        const uint64_t row0 = first / pieces;
+        const uint32_t in = (uint32_t)(first - row0 * pieces) + threadIdx.x;
+        const int64_t t = (int64_t)(row0 + in / pieces);
+        if (t < a.T) gate_grad_piece<DT>(a, t, (int64_t)(in % pieces) * 8);
+    }
+}
+
+// The workgroups of `pieces` threads: those of a launch have to be below 2^32 threads, the others are walked
+static uint32_t workgroups(int64_t pieces) { return (uint32_t)((pieces + 255) / 256 < (1 << 22) ? (pieces + 255) / 256 : 1 << 22); }
+
 int launch_gate_grad(const GateArgs& a, int dtype, void* stream) {
-    const int64_t threads = a.T * (a.cols / 8), grid = (threads + 255) / 256;
-    if (grid > INT32_MAX) return 1;
-    if (dtype == FEED_F32) hipLaunchKernelGGL(gate_grad_kernel<FEED_F32>, dim3((uint32_t)grid), dim3(256), 0, (hipStream_t)stream, a);
-    else hipLaunchKernelGGL(gate_grad_kernel<FEED_BF16>, dim3((uint32_t)grid), dim3(256), 0, (hipStream_t)stream, a);
+    const dim3 grid(workgroups(a.T * (a.cols / 8)));
+    if (dtype == FEED_F32) hipLaunchKernelGGL(gate_grad_kernel<FEED_F32>, grid, dim3(256), 0, (hipStream_t)stream, a);
+    else hipLaunchKernelGGL(gate_grad_kernel<FEED_BF16>, grid, dim3(256), 0, (hipStream_t)stream, a);
     return hipGetLastError() == hipSuccess ? 0 : 1;
 }
 
 // ---- arrays whose rows 16-byte loads cannot start with, to rows where they can: a piece of 16 bytes a thread
-__global__ void __launch_bounds__(256) pad_kernel(const PadArgs a) {
-    const uint32_t pieces = (uint32_t)(a.ld / 16);
-    const uint64_t first = (uint64_t)blockIdx.x * 256, row0 = first / pieces;
-    const uint32_t in = (uint32_t)(first - row0 * pieces) + threadIdx.x;
-    int64_t row = (int64_t)(row0 + in / pieces);
-    const int64_t at = (int64_t)(in % pieces) * 16;
+__device__ __forceinline__ void pad_piece(const PadArgs& a, int64_t row, int64_t at) {
     char* const to = a.to + row * a.ld + at;
     int i = 0;
     while (i < 3 && row >= a.rows[i]) row -= a.rows[i++];
-    if (i == 3) return;
+    if (i == 3) return;                                      // (threads behind the last row)
     const char* const from = (i == 0 ? a.from[0] : i == 1 ? a.from[1] : a.from[2]) + row * (i == 0 ? a.ld_from[0] : i == 1 ? a.ld_from[1] : a.ld_from[2]) + at;
     eu32x4 v = {0, 0, 0, 0};
     if (at + 16 <= a.bytes) {
@@ -227,11 +229,19 @@ __global__ void __launch_bounds__(256) pad_kernel(const PadArgs a) {
     }
     *(eu32x4*)to = v;
 }
+__global__ void __launch_bounds__(256) pad_kernel(const PadArgs a) {
+    const uint32_t pieces = (uint32_t)(a.ld / 16);
+    const uint64_t all = (uint64_t)(a.rows[0] + a.rows[1] + a.rows[2]) * pieces;
+    for (uint64_t first = (uint64_t)blockIdx.x * 256; first < all; first += (uint64_t)gridDim.x * 256) {
+        const uint64_t row0 = first / pieces;
+        const uint32_t in = (uint32_t)(first - row0 * pieces) + threadIdx.x;
+        pad_piece(a, (int64_t)(row0 + in / pieces), (int64_t)(in % pieces) * 16);
+    }
+}
 
 int launch_pad(const PadArgs& a, void* stream) {
-    const int64_t grid = ((a.rows[0] + a.rows[1] + a.rows[2]) * (a.ld / 16) + 255) / 256;
-    if (grid > INT32_MAX) return 1;
-    if (grid > 0) hipLaunchKernelGGL(pad_kernel, dim3((uint32_t)grid), dim3(256), 0, (hipStream_t)stream, a);
+    const int64_t pieces = (a.rows[0] + a.rows[1] + a.rows[2]) * (a.ld / 16);
+    if (pieces > 0) hipLaunchKernelGGL(pad_kernel, dim3(workgroups(pieces)), dim3(256), 0, (hipStream_t)stream, a);
     return hipGetLastError() == hipSuccess ? 0 : 1;
 }
 

@@ -911,7 +911,8 @@ template <int DT, int FORM>
 static int launch_form(const FeedArgs& a, void* stream) {
     constexpr bool Q_STRIDED = FORM == FEED_BOTH, P_STRIDED = FORM >= FEED_RIGHT;
     const int size = feed_size(DT);
-    const bool q = direct(a.q[0], size, Q_STRIDED), p = direct(a.p[0], size, P_STRIDED) && (FORM != FEED_GATED && FORM != FEED_RIGHT || direct(a.p[1], size, P_STRIDED));
+    constexpr bool TWO = FORM == FEED_GATED || FORM == FEED_RIGHT;
+    const bool q = direct(a.q[0], size, Q_STRIDED), p = direct(a.p[0], size, P_STRIDED) && (!TWO || direct(a.p[1], size, P_STRIDED));
     if constexpr (FORM >= FEED_RIGHT) return p ? launch_shape<DT, FORM, true, true>(a, stream) : launch_shape<DT, FORM, true, false>(a, stream);
     else return q && p ? launch_shape<DT, FORM, true, true>(a, stream) : launch_shape<DT, FORM, false, false>(a, stream);
 }

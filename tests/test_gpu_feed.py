@@ -101,6 +101,20 @@ def test_matmul_scaled(env, T, C, K, pad, shift, out):
     y.check()
 
 
+@pytest.mark.parametrize("out", ["f32", "bf16"])
+@pytest.mark.parametrize("T", [2, 300])
+def test_every_8_bit_number(env, T, out):
+    """Each of the 254 finite numbers, subnormal ones among them, times one: bf16 holds them all."""
+    cc, torch = env
+    x = torch.arange(254, dtype=torch.uint8)
+    x = torch.where(x < 127, x, x + 1).view(2, 127).repeat(T // 2, 1)
+    w = torch.where(torch.eye(127, dtype=torch.bool), 0x38, 0).to(torch.uint8)      # 0x38 is 1
+    y = torch.zeros((T, 127), dtype=typ(torch, out), device="cuda")
+    one = lambda n: torch.ones((n, 1), device="cuda")  # noqa: E731
+    cc.cacnn_matmul_scaled((T, 127, 127), x.cuda(), one(T), w.cuda(), one(1), code(cc, out), y)
+    assert np.array_equal(y.cpu().double().numpy(), feed.e4m3_values()[x.numpy()])
+
+
 def test_a_nan_stays_in_its_row_and_column(env):
     cc, torch = env
     rng = np.random.default_rng(5)

@@ -44,7 +44,7 @@ REFUSED = [
     (forward, NULL, [dict(x=None), dict(wg=None), dict(wu=None), dict(out=None)]),
     (forward, UNSUPPORTED, [dict(dtype=2), dict(act=3), dict(act=-1)]),
     (forward, INVALID, [dict(T=-1), dict(C=0), dict(F=0), dict(F=BIG), dict(ld_x=255), dict(ld_w=-1), dict(ld_out=63), dict(gate=A), dict(up=A), dict(x=A + 1),
-                        dict(gate=A + 1, up=A), dict(dtype=0, wg=A + 2), dict(gate=A, up=A, ld_pre=32)]),
+                        dict(gate=A + 1, up=A), dict(dtype=0, wg=A + 2), dict(gate=A, up=A, ld_pre=32), dict(T=(1 << 31) - 1, F=64, C=1 << 20), dict(F=1 << 20, C=1 << 20)]),
     (forward_scaled, NULL, [dict(x=None), dict(xs=None), dict(wg=None), dict(gs=None), dict(wu=None), dict(us=None), dict(out=None)]),
     (forward_scaled, UNSUPPORTED, [dict(out_dtype=2), dict(act=9)]),
     (forward_scaled, INVALID, [dict(C=0), dict(T=-5), dict(xs=A + 2), dict(us=A + 2), dict(out=A + 1), dict(ld_w=7)]),
@@ -174,8 +174,9 @@ def test_more_that_does_not_fit(calls):
     grads = dict(x=on(4, 256), w_gate=on(64, 256), w_up=on(64, 256), grad_out=on(4, 64), grad_x=on(4, 256), grad_w_gate=None, grad_w_up=None)
     with pytest.raises(ValueError, match="workspace"):
         cc.cacnn_gated_backward((4, 256, 64, 0), 1, **grads, workspace=torch.zeros(4096, dtype=torch.uint8))
-    with pytest.raises(ValueError, match="workspace"):
-        cc.cacnn_gated_backward((4, 256, 64, 0), 1, **grads, workspace=on(64, 64, dtype=torch.uint8).t())
+    for work in (on(64, 64, dtype=torch.uint8).t(), None, 4096):
+        with pytest.raises(ValueError, match="workspace"):
+            cc.cacnn_gated_backward((4, 256, 64, 0), 1, **grads, workspace=work)
     assert not calls
 
 
