@@ -37,12 +37,12 @@ int64_t padded(int64_t n) { return (n + 63) / 64 * 64; }      // columns of a ro
 
 // The workspace of the backward pass: the gradients of gate and up, and, where rows of C elements are no multiple of 16 bytes, X and both weights with rows
 // that are: the products read them two and three times each, and faster straight to LDS (bf16 (2048, 2047, 4095) 490 us in all without the copies, 289 with them).
-// Not for few rows, where the copies would be most of the traffic.
+// Not for few rows, where the copies would be most of the traffic, unless C is too short for a 16-byte load.
 struct Workspace {
     int64_t ld_f, ld_c;            // elements of a row; ld_c 0: no copies
     int64_t grad, x, w;            // bytes of grad_gate (and of grad_up), of the copies of X and of a weight
     Workspace(const cacnn_gated_problem& p, int size)
-        : ld_f(padded(p.F)), ld_c(p.C * size % 16 && p.T >= 128 ? padded(p.C) : 0), grad(p.T * ld_f * size), x(p.T * ld_c * size), w(p.F * ld_c * size) {}
+        : ld_f(padded(p.F)), ld_c(p.C * size < 16 || (p.C * size % 16 && p.T >= 128) ? padded(p.C) : 0), grad(p.T * ld_f * size), x(p.T * ld_c * size), w(p.F * ld_c * size) {}
     int64_t bytes() const { return 2 * grad + x + 2 * w; }
 };
 
@@ -259,7 +259,10 @@ int cacnn_gated_backward(const cacnn_gated_problem* problem, int dtype, const vo
         a.M = p.T, a.N = p.C;
         if (launch_matmul(a, FEED_RIGHT, dtype, hip_stream) != 0) return CACNN_ERR_LAUNCH;
     }
-    if (grad_w_gate) {
+    if (grad_w_gate && p.T == 0) {
+        for (void* const w : {grad_w_gate, grad_w_up})
+            if (launch_zeros(output(w, p.ld_grad_w, size), p.F, p.C, hip_stream) != 0) return CACNN_ERR_LAUNCH;
+    } else if (grad_w_gate) {
         FeedArgs a = {};
         a.segments = 1, a.products = 2;
         a.q[0] = operand(grad_gate, ld, size, p.F, p.T, true), a.q[1] = operand(grad_up, ld, size, p.F, p.T, true);

@@ -91,6 +91,8 @@ struct PadArgs {
     int32_t size;              // of an element
 };
 int launch_pad(const PadArgs& a, void* stream);
+// rows x cols elements of `o` become zeros
+int launch_zeros(const FeedOut& o, int64_t rows, int64_t cols, void* stream);
 
 struct QuantizeArgs {
     const char* x;

@@ -245,4 +245,16 @@ int launch_pad(const PadArgs& a, void* stream) {
     return hipGetLastError() == hipSuccess ? 0 : 1;
 }
 
+__global__ void __launch_bounds__(256) zeros_kernel(const FeedOut o, int64_t rows, int64_t cols) {
+    for (int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x; t < rows * cols; t += (int64_t)gridDim.x * 256) {
+        char* const p = o.base + t / cols * o.ld + t % cols * o.size;
+        if (o.size == 4) *(uint32_t*)p = 0;
+        else *(uint16_t*)p = 0;
+    }
+}
+int launch_zeros(const FeedOut& o, int64_t rows, int64_t cols, void* stream) {
+    hipLaunchKernelGGL(zeros_kernel, dim3(workgroups(rows * cols)), dim3(256), 0, (hipStream_t)stream, o, rows, cols);
+    return hipGetLastError() == hipSuccess ? 0 : 1;
+}
+
 }  // namespace cacnn

@@ -81,91 +81,67 @@ __device__ __forceinline__ mu32x4 moved_down(mu32x4 v, int bytes) {
                   __builtin_amdgcn_alignbyte(0, v[3], b)};
 }
 
-// Brings slabs to LDS through registers, from any address and of any size, 16 bytes a load.  A piece that the end of a row cuts is loaded as the row's
-// last 16 bytes and moved down when it has come; what lies behind the last contraction index becomes zeros, rows and columns behind the last stand for
-// it again (what comes of them is not stored).  Rows of less than 16 bytes are read element by element.
-// (With the cut pieces read element by element the tiles at the edge took as long as all others together: bf16 (2048, 2047, 4095), the gradient
-// of x, 577 us then and 198 now.)
-template <int ESZ, bool STRIDED, int ROWS, int WAVES, int SLAB>
+// Brings slabs to LDS through registers, from any address, 16 bytes a load, where rows have 16 bytes or more.  Every load is made, and within the array: a
+// piece that the end of a row cuts is loaded as the row's last 16 bytes and moved down when it has come, all the way where it lies behind the last
+// contraction index; rows and columns behind the last stand for it again (what comes of them is not stored).  (With a question before each load
+// the compiler waits for all that are on their way before it uses one, and with the cut pieces read element by element the tiles at the edge took as
+// long as all others together.)
+// SETS of registers: slabs on their way at a time; which set a slab has is known where it is loaded and put.
+template <int ESZ, bool STRIDED, int ROWS, int WAVES, int SLAB, int SETS>
 struct RegisterLoader {
     using Map = SlabMap<ESZ, STRIDED, ROWS, WAVES, SLAB>;
     const char* base;
     int64_t ld, k;
     int rows, wave, lane;
-    bool tiny, cut;                // rows of less than 16 bytes; the last slab's pieces have to be moved
-    int off[Map::N];               // (in a tile of few columns the row's last 16 bytes begin before it)
-    int down[Map::N], edge[Map::N];    // bytes to move the slab's pieces by, and (strided) those at the last column
-    mu32x4 r[Map::N];
+    bool cut[SETS];                // the slab's pieces have to be moved
+    int off[Map::N];               // (strided, in a tile of few columns: the row's last 16 bytes begin before it)
+    int down[SETS][Map::N], edge[Map::N];    // bytes to move the slab's pieces by, and (strided) those at the last column
+    mu32x4 r[SETS][Map::N];
 
     __device__ __forceinline__ void init(const FeedOperand& o, int64_t row0, int wave_, int lane_) {
         ld = o.ld, k = o.k, wave = wave_, lane = lane_;
         rows = (int)max((int64_t)0, min((int64_t)ROWS, o.rows - row0));
-        tiny = (STRIDED ? o.rows : k) * ESZ < 16;
         move(o, row0);
 #pragma unroll
         for (int i = 0; i < Map::N; ++i) {
             edge[i] = 0;
             if constexpr (STRIDED) {
-                const int col = Map::column(i, wave, lane), left = rows * ESZ - col;
-                edge[i] = left >= 16 || tiny ? 0 : left > 0 ? 16 - left : 16;
-                off[i] = Map::index(i, wave, lane) * (int)ld + (left >= 16 || tiny ? col : rows * ESZ - 16);
+                const int col = Map::column(i, wave, lane), last = rows ? rows * ESZ - 16 : 0;
+                edge[i] = min(max(col - last, 0), 16);
+                off[i] = Map::index(i, wave, lane) * (int)ld + min(col, last);
             } else {
-                off[i] = min(Map::row(i, wave, lane), max(rows - 1, 0)) * (int)ld + Map::byte(i, wave, lane);
+                off[i] = min(Map::row(i, wave, lane), max(rows - 1, 0)) * (int)ld;
             }
         }
     }
-    __device__ __forceinline__ void move(const FeedOperand& o, int64_t row0) { base = o.base + (STRIDED ? row0 * ESZ : row0 * ld); }
+    // (a tile behind the last row or column: the first ones')
+    __device__ __forceinline__ void move(const FeedOperand& o, int64_t row0) { base = o.base + (rows ? (STRIDED ? row0 * ESZ : row0 * ld) : 0); }
     // slab s of the operand (none if !any: zeros)
-    __device__ __forceinline__ void load(int64_t s, bool any) {
-        const char* const from = base + (STRIDED ? s * Map::KR * ld : s * SLAB);
+    __device__ __forceinline__ void load(int64_t s, bool any, int set) {
         any = any && rows > 0;
-        cut = STRIDED && rows < ROWS;
-        if (any && !tiny && (STRIDED ? (s + 1) * Map::KR <= k : (s + 1) * SLAB <= k * ESZ)) {
-#pragma unroll
-            for (int i = 0; i < Map::N; ++i) {
-                down[i] = edge[i];
-                r[i] = ((const MatBytes16*)(from + off[i]))->v;
-            }
-            return;
-        }
-        cut = true;
+        cut[set] = !any || (STRIDED ? rows < ROWS || (s + 1) * Map::KR > k : (s + 1) * SLAB > k * ESZ);
+        const char* const from = base + (STRIDED ? s * Map::KR * ld : 0);
+        const int left = (int)min(k - s * Map::KR, (int64_t)Map::KR);             // strided: indices from the slab's first to the operand's last
+        const int end = (int)(k * ESZ);
 #pragma unroll
         for (int i = 0; i < Map::N; ++i) {
-            r[i] = mu32x4{0, 0, 0, 0};
-            down[i] = 0;
-            if (!any) continue;
-            if (tiny) {
-                // elements of this piece that belong to the operand
-                int64_t left;
-                if constexpr (STRIDED) left = s * Map::KR + Map::index(i, wave, lane) < k ? rows * ESZ - Map::column(i, wave, lane) : 0;
-                else left = Map::row(i, wave, lane) < rows ? k * ESZ - s * SLAB - Map::byte(i, wave, lane) : 0;
-#pragma unroll
-                for (int e = 0; e < 16 / ESZ; ++e)
-                    if (e * ESZ < left) {
-                        const char* const p = from + off[i];
-                        uint32_t x;
-                        if constexpr (ESZ == 4) x = *(const uint32_t*)(p + e * 4);
-                        else if constexpr (ESZ == 2) x = *(const uint16_t*)(p + e * 2);
-                        else x = *(const uint8_t*)(p + e);
-                        r[i][e * ESZ / 4] |= x << (e * ESZ % 4 * 8);
-                    }
-            } else if constexpr (STRIDED) {
-                const bool there = s * Map::KR + Map::index(i, wave, lane) < k;
-                down[i] = there ? edge[i] : 16;
-                if (there) r[i] = ((const MatBytes16*)(from + off[i]))->v;
+            if constexpr (STRIDED) {
+                const int behind = max(Map::index(i, wave, lane) - left + 1, 0);
+                down[set][i] = any && !behind ? edge[i] : 16;
+                r[set][i] = ((const MatBytes16*)(from + (off[i] - behind * (int)ld)))->v;
             } else {
-                const int left = (int)(k * ESZ - s * SLAB) - Map::byte(i, wave, lane);
-                down[i] = left >= 16 ? 0 : left > 0 ? 16 - left : 16;
-                if (left > 0) r[i] = ((const MatBytes16*)(from + off[i] - down[i]))->v;
+                const int at = (int)s * SLAB + Map::byte(i, wave, lane), to = min(at, end - 16);
+                down[set][i] = any ? min(at - to, 16) : 16;
+                r[set][i] = ((const MatBytes16*)(from + (off[i] + to)))->v;
             }
         }
     }
-    __device__ __forceinline__ void put(char* slab) {
-        if (cut)
+    __device__ __forceinline__ void put(char* slab, int set) {
+        if (cut[set])
 #pragma unroll
-            for (int i = 0; i < Map::N; ++i) r[i] = moved_down(r[i], down[i]);
+            for (int i = 0; i < Map::N; ++i) r[set][i] = moved_down(r[set][i], down[set][i]);
 #pragma unroll
-        for (int i = 0; i < Map::N; ++i) *(mu32x4*)(slab + (i * WAVES + wave) * 1024 + lane * 16) = r[i];
+        for (int i = 0; i < Map::N; ++i) *(mu32x4*)(slab + (i * WAVES + wave) * 1024 + lane * 16) = r[set][i];
     }
 };
 
@@ -238,26 +214,26 @@ __device__ __forceinline__ void loads_done() { asm volatile("s_waitcnt vmcnt(0)"
 __device__ __forceinline__ void lds_done() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
 
 // One operand's way to LDS
-template <int ESZ, bool STRIDED, int ROWS, int WAVES, int SLAB, bool DIRECT>
+template <int ESZ, bool STRIDED, int ROWS, int WAVES, int SLAB, bool DIRECT, int SETS>
 struct Loader {
     static constexpr int LOADS = SlabMap<ESZ, STRIDED, ROWS, WAVES, SLAB>::N;
     DirectLoader<ESZ, STRIDED, ROWS, WAVES, SLAB> l;
     __device__ __forceinline__ void init(const FeedOperand& o, int64_t row0, int wave, int lane) { l.init(o, row0, wave, lane); }
     __device__ __forceinline__ void move(const FeedOperand& o, int64_t row0) { l.move(o, row0); }
     // slab s is brought by the LOADS calls of issue() that follow, or by put() after the loads that prepare() made have come
-    __device__ __forceinline__ void prepare(int s, bool any) { l.prepare(s, any); }
+    __device__ __forceinline__ void prepare(int s, bool any, int) { l.prepare(s, any); }
     __device__ __forceinline__ void issue(int i, uint32_t slab) { l.issue(i, slab); }
-    __device__ __forceinline__ void put(char*) {}
+    __device__ __forceinline__ void put(char*, int) {}
 };
-template <int ESZ, bool STRIDED, int ROWS, int WAVES, int SLAB>
-struct Loader<ESZ, STRIDED, ROWS, WAVES, SLAB, false> {
+template <int ESZ, bool STRIDED, int ROWS, int WAVES, int SLAB, int SETS>
+struct Loader<ESZ, STRIDED, ROWS, WAVES, SLAB, false, SETS> {
     static constexpr int LOADS = 0;
-    RegisterLoader<ESZ, STRIDED, ROWS, WAVES, SLAB> l;
+    RegisterLoader<ESZ, STRIDED, ROWS, WAVES, SLAB, SETS> l;
     __device__ __forceinline__ void init(const FeedOperand& o, int64_t row0, int wave, int lane) { l.init(o, row0, wave, lane); }
     __device__ __forceinline__ void move(const FeedOperand& o, int64_t row0) { l.move(o, row0); }
-    __device__ __forceinline__ void prepare(int s, bool any) { l.load(s, any); }
+    __device__ __forceinline__ void prepare(int s, bool any, int set) { l.load(s, any, set); }
     __device__ __forceinline__ void issue(int, uint32_t) {}
-    __device__ __forceinline__ void put(char* slab) { l.put(slab); }
+    __device__ __forceinline__ void put(char* slab, int set) { l.put(slab, set); }
 };
 
 // A block of 32 rows (or columns) of step `st` of a slab, as the matrix instructions take it: 16 bytes a lane
@@ -425,8 +401,10 @@ __global__ void __launch_bounds__(WM* WN * 64, WM* WN == 4 ? 2 : 1) matmul_block
     const TilePlace at = tile_place(a, blockIdx.x);
     const int64_t m0 = (int64_t)at.m * S::BM, n0 = (int64_t)at.n * S::COLS;
 
-    using QLoader = Loader<ESZ, S::Q_STRIDED, S::BM, WAVES, SLAB, QD>;
-    using PLoader = Loader<ESZ, S::P_STRIDED, S::P_ROWS, WAVES, SLAB, PD>;
+    // (both through registers: two slabs on their way.  With one, a slab took as long as its loads: bf16 gated (777, 1001, 1515) 25.5 us)
+    constexpr int SETS = !QD && !PD && ESZ > 1 ? 2 : 1;
+    using QLoader = Loader<ESZ, S::Q_STRIDED, S::BM, WAVES, SLAB, QD, SETS>;
+    using PLoader = Loader<ESZ, S::P_STRIDED, S::P_ROWS, WAVES, SLAB, PD, SETS>;
     constexpr int LOADS = QLoader::LOADS + S::P_PARTS * PLoader::LOADS + (ESZ == 1 ? 1 : 0);    // of a wave and slab
     QLoader q;
     PLoader p0, p1;                                            // (p1: of up, where there is one)
@@ -443,7 +421,7 @@ __global__ void __launch_bounds__(WM* WN * 64, WM* WN == 4 ? 2 : 1) matmul_block
     const uint32_t lds = lds_address(s_mem);
     uint32_t coming = lds;
     int coming_slab = 0;
-    auto prepare = [&](int s, int at_stage) MAT_INLINE {
+    auto prepare = [&](int s, int at_stage, int set) MAT_INLINE {
         coming = lds + at_stage * S::STAGE;
         coming_slab = s;
         if constexpr (FORM == FEED_RIGHT)
@@ -453,9 +431,9 @@ __global__ void __launch_bounds__(WM* WN * 64, WM* WN == 4 ? 2 : 1) matmul_block
                 p0.move(a.p[1], n0);
             }
         const bool any = s < slabs && coming_slab < per_segment;
-        q.prepare(coming_slab, any);
-        p0.prepare(coming_slab, any);
-        if constexpr (S::GATED) p1.prepare(coming_slab, any);
+        q.prepare(coming_slab, any, set);
+        p0.prepare(coming_slab, any, set);
+        if constexpr (S::GATED) p1.prepare(coming_slab, any, set);
     };
     auto load_some = [&](int from, int to) MAT_INLINE {
 #pragma unroll
@@ -473,11 +451,11 @@ __global__ void __launch_bounds__(WM* WN * 64, WM* WN == 4 ? 2 : 1) matmul_block
                     load_word_to_lds_unseen(scales, scale_off + coming_slab * 4, coming + S::Q_BYTES + S::P_BYTES + scale_wave * 256);
         }
     };
-    auto put = [&](int at_stage) MAT_INLINE {
+    auto put = [&](int at_stage, int set) MAT_INLINE {
         char* const stage = s_mem + at_stage * S::STAGE;
-        q.put(stage);
-        p0.put(stage + S::Q_BYTES);
-        if constexpr (S::GATED) p1.put(stage + S::Q_BYTES + S::P_ROWS * SLAB);
+        q.put(stage, set);
+        p0.put(stage + S::Q_BYTES, set);
+        if constexpr (S::GATED) p1.put(stage + S::Q_BYTES + S::P_ROWS * SLAB, set);
     };
     // a wave's i-th block of columns: part of p, block within it
     auto part_of = [&](int i) { return S::GATED ? i / (PB / 2) : 0; };
@@ -486,14 +464,14 @@ __global__ void __launch_bounds__(WM* WN * 64, WM* WN == 4 ? 2 : 1) matmul_block
     auto q_slab = [&](int at_stage) -> const char* { return s_mem + at_stage * S::STAGE; };
     auto p_slab = [&](int at_stage, int i) -> const char* { return s_mem + at_stage * S::STAGE + S::Q_BYTES + part_of(i) * S::P_ROWS * SLAB; };
     // This wave has read what it needs of slab s - 1, and slab s is there for all; the stage of slab s - 1 takes the next one
-    auto next = [&](int s) MAT_INLINE {
+    auto next = [&](int s, int set) MAT_INLINE {
         const int free = stage;
         stage = stage + 1 == STAGES ? 0 : stage + 1;
-        asm volatile("s_waitcnt vmcnt(%0)" ::"n"((STAGES - 2) * LOADS) : "memory");
-        put(stage);
+        if constexpr (LOADS > 0) asm volatile("s_waitcnt vmcnt(%0)" ::"n"((STAGES - 2) * LOADS) : "memory");
+        put(stage, set);
         lds_done();
         __builtin_amdgcn_s_barrier();
-        prepare(s + STAGES - 1, free);
+        prepare(s + (SETS > 1 ? SETS : STAGES - 1), free, set);
         asm volatile("" ::: "memory");
     };
     // Between two calls of next() the wave multiplies several times, and behind each brings a part of the next slab: all at once, the loads keep it
@@ -513,12 +491,12 @@ __global__ void __launch_bounds__(WM* WN * 64, WM* WN == 4 ? 2 : 1) matmul_block
             for (int v = 0; v < 16; ++v) acc[i][h][v] = 0.f;
 
 #pragma unroll
-    for (int s = 0; s < STAGES - 1; ++s) {
-        prepare(s, s);
+    for (int s = 0; s < (SETS > 1 ? SETS : STAGES - 1); ++s) {
+        prepare(s, s, SETS > 1 ? s : 0);
         load_some(0, LOADS);
     }
     stage = STAGES - 1;
-    next(0);
+    next(0, 0);
     if constexpr (DT == FEED_E4M3) load_some(0, phase_of(1, QB));
     if constexpr (DT == FEED_E4M3_EXACT) load_some(0, LOADS);
     if constexpr (ESZ > 1) {
@@ -545,18 +523,22 @@ __global__ void __launch_bounds__(WM* WN * 64, WM* WN == 4 ? 2 : 1) matmul_block
         read(0, 0);
         // (the first slab's phases but the last, which is the first one's behind next())
         load_some(0, phase_of(PB, PB * STEPS));
-        for (int s = 0; s < slabs; ++s) {
+        for (int from = 0; from < slabs; from += SETS)
 #pragma unroll
-            for (int st = 0; st < STEPS; ++st) {
-                if (st + 1 < STEPS) {
-                    read(st + 1, (st + 1) & 1);
-                } else if (s + 1 < slabs) {
-                    next(s + 1);
-                    read(0, 0);
+            for (int set = 0; set < SETS; ++set) {
+                const int s = from + set;
+                if (set > 0 && s >= slabs) break;
+#pragma unroll
+                for (int st = 0; st < STEPS; ++st) {
+                    if (st + 1 < STEPS) {
+                        read(st + 1, (st + 1) & 1);
+                    } else if (s + 1 < slabs) {
+                        next(s + 1, (set + 1) % SETS);
+                        read(0, 0);
+                    }
+                    products(st & 1, (st + 1) % STEPS);
                 }
-                products(st & 1, (st + 1) % STEPS);
             }
-        }
     } else {
         for (int s = 0; s < slabs; ++s) {
             // a slab is one block of the scales: its sum of products first, then the product of the two scales times it
@@ -595,7 +577,7 @@ __global__ void __launch_bounds__(WM* WN * 64, WM* WN == 4 ? 2 : 1) matmul_block
                 read_q(0);
 #pragma unroll
                 for (int h = 0; h < QB; ++h) {
-                    if (h + 1 == QB && s + 1 < slabs) next(s + 1);
+                    if (h + 1 == QB && s + 1 < slabs) next(s + 1, 0);
                     mf32x16 c[PB];
 #pragma unroll
                     for (int i = 0; i < PB; ++i) {
@@ -637,7 +619,7 @@ __global__ void __launch_bounds__(WM* WN * 64, WM* WN == 4 ? 2 : 1) matmul_block
 #pragma unroll
                     for (int h = 0; h < QB; ++h) add(i, h, c[i][h]);
                 if (s + 1 < slabs) {
-                    next(s + 1);
+                    next(s + 1, 0);
                     load_some(0, LOADS);
                 }
             }
@@ -702,8 +684,9 @@ __global__ void __launch_bounds__(256) matmul_waves_kernel(const FeedArgs a) {
     const int64_t m0 = (int64_t)at.m * S::BM, n0 = (int64_t)at.n * S::COLS;
     char* const mine = s_mem + wave * (S::DEPTH * S::STAGE);
 
-    Loader<ESZ, S::Q_STRIDED, S::BM, 1, SLAB, QD> q;
-    Loader<ESZ, S::P_STRIDED, S::P_ROWS, 1, SLAB, PD> p[S::P_PARTS];
+    constexpr int SETS = !QD && !PD && ESZ > 1 ? 2 : 1;        // (as above)
+    Loader<ESZ, S::Q_STRIDED, S::BM, 1, SLAB, QD, SETS> q;
+    Loader<ESZ, S::P_STRIDED, S::P_ROWS, 1, SLAB, PD, SETS> p[S::P_PARTS];
     q.init(a.q[at.product], m0, 0, lane);
 #pragma unroll
     for (int h = 0; h < S::P_PARTS; ++h) p[h].init(a.p[h], n0, 0, lane);
@@ -712,7 +695,7 @@ __global__ void __launch_bounds__(256) matmul_waves_kernel(const FeedArgs a) {
     const uint32_t scale_off = (uint32_t)lane * a.scale_cols * 4;
     int segment = 0;
     // the wave's slab of turn `i` into stage `stage`; none behind the last: zeros, so that the loads on their way can be counted
-    auto begin = [&](int i, int stage) MAT_INLINE {
+    auto begin = [&](int i, int stage, int set) MAT_INLINE {
         const int s = i * 4 + wave;
         const uint32_t to = lds_address(mine) + stage * S::STAGE;
         int x = s;
@@ -725,22 +708,22 @@ __global__ void __launch_bounds__(256) matmul_waves_kernel(const FeedArgs a) {
                     p[0].move(a.p[1], n0);
                 }
             }
-        q.prepare(x, s < slabs);
+        q.prepare(x, s < slabs, set);
 #pragma unroll
         for (int l = 0; l < S::BM / 8; ++l) q.issue(l, to);
 #pragma unroll
         for (int h = 0; h < S::P_PARTS; ++h) {
-            p[h].prepare(x, s < slabs);
+            p[h].prepare(x, s < slabs, set);
 #pragma unroll
             for (int l = 0; l < S::P_ROWS / 8; ++l) p[h].issue(l, to + S::Q_BYTES + h * S::P_ROWS * SLAB);
         }
         if constexpr (ESZ == 1) load_word_to_lds_unseen(scales, scale_off + x * 4, to + S::Q_BYTES + S::P_BYTES);
     };
-    auto put = [&](int stage) MAT_INLINE {
+    auto put = [&](int stage, int set) MAT_INLINE {
         char* const to = mine + stage * S::STAGE;
-        q.put(to);
+        q.put(to, set);
 #pragma unroll
-        for (int h = 0; h < S::P_PARTS; ++h) p[h].put(to + S::Q_BYTES + h * S::P_ROWS * SLAB);
+        for (int h = 0; h < S::P_PARTS; ++h) p[h].put(to + S::Q_BYTES + h * S::P_ROWS * SLAB, set);
     };
     auto part_of = [&](int i) { return S::GATED ? i / (PB / 2) : 0; };
     auto block_of = [&](int i) { return S::GATED ? i % (PB / 2) : i; };
@@ -801,27 +784,41 @@ __global__ void __launch_bounds__(256) matmul_waves_kernel(const FeedArgs a) {
 
     if constexpr (QD && PD) {
 #pragma unroll
-        for (int i = 0; i < DEPTH - 1; ++i) begin(i, i);
+        for (int i = 0; i < DEPTH - 1; ++i) begin(i, i, 0);
         int stage = 0, free = DEPTH - 1;
         for (int i = 0; i < turns; ++i) {
             lds_done();                                    // what was read of the stage that is filled now
-            begin(i + DEPTH - 1, free);
+            begin(i + DEPTH - 1, free, 0);
             asm volatile("s_waitcnt vmcnt(%0)" ::"n"((DEPTH - 1) * S::LOADS) : "memory");
             if (i * 4 + wave < slabs) compute(i * 4 + wave, stage);
             free = stage;
             stage = stage + 1 == DEPTH ? 0 : stage + 1;
         }
+    } else if constexpr (SETS == 2) {
+        begin(0, 0, 0);
+        begin(1, 1, 1);
+        put(0, 0);
+        begin(2, 0, 0);
+        for (int from = 0; from < turns; from += 2)
+#pragma unroll
+            for (int set = 0; set < 2; ++set) {
+                const int i = from + set;
+                if (set > 0 && i >= turns) break;
+                if (i * 4 + wave < slabs) compute(i * 4 + wave, set);
+                put(1 - set, 1 - set);
+                begin(i + 3, 1 - set, 1 - set);
+            }
     } else {
-        begin(0, 0);
+        begin(0, 0, 0);
         loads_done();
-        put(0);
+        put(0, 0);
         for (int i = 0; i < turns; ++i) {
             lds_done();
-            begin(i + 1, (i + 1) & 1);
+            begin(i + 1, (i + 1) & 1, 0);
             asm volatile("" ::: "memory");
             if (i * 4 + wave < slabs) compute(i * 4 + wave, i & 1);
             loads_done();
-            put((i + 1) & 1);
+            put((i + 1) & 1, 0);
         }
     }
     loads_done();
@@ -853,6 +850,33 @@ __global__ void __launch_bounds__(256) matmul_waves_kernel(const FeedArgs a) {
             sum(S::GATED ? i + PB / 2 : i, h, u);
             finish_run<DT, S::GATED>(a, at.product, m0 + h * 32 + j, n0 + block_of(i) * 32 + wave * 8 + g * 4, v, u);
         }
+}
+
+// Contractions of less than 16 bytes: four columns of a row a thread, element by element
+template <int DT, bool GATED>
+__global__ void __launch_bounds__(256) matmul_short_kernel(const FeedArgs a) {
+    auto element = [](const char* p, int64_t i) -> float {
+        if constexpr (DT == FEED_F32) return ((const float*)p)[i];
+        else if constexpr (DT == FEED_BF16) return __uint_as_float((uint32_t)((const uint16_t*)p)[i] << 16);
+        else return __builtin_amdgcn_cvt_f32_fp8(((const uint8_t*)p)[i], 0);
+    };
+    const int64_t fours = (a.N + 3) / 4;
+    for (int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x; t < a.M * fours; t += (int64_t)gridDim.x * 256) {
+        const int64_t m = t / fours, n = t % fours * 4;
+        float sum[2][4];
+#pragma unroll
+        for (int h = 0; h < (GATED ? 2 : 1); ++h)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                float x = 0.f;
+                if (n + e < a.N)
+                    for (int64_t i = 0; i < a.q[0].k; ++i)
+                        x = __builtin_fmaf(element(a.q[0].base + m * a.q[0].ld, i), element(a.p[h].base + (n + e) * a.p[h].ld, i), x);
+                if (feed_size(DT) == 1 && n + e < a.N) x *= a.q_scale[m] * a.p_scale[h][(n + e) / kScaleBlock];
+                sum[h][e] = x;
+            }
+        finish_run<DT, GATED>(a, 0, m, n, sum[0], sum[GATED ? 1 : 0]);
+    }
 }
 
 // One launch of a kernel whose workgroups own S::BM x S::COLS of Out
@@ -912,6 +936,12 @@ static int launch_form(const FeedArgs& a, void* stream) {
     constexpr bool Q_STRIDED = FORM == FEED_BOTH, P_STRIDED = FORM >= FEED_RIGHT;
     const int size = feed_size(DT);
     constexpr bool TWO = FORM == FEED_GATED || FORM == FEED_RIGHT;
+    if constexpr (FORM == FEED_GATED || FORM == FEED_PLAIN)
+        if (a.q[0].k * size < 16 && !a.q[0].padded) {
+            const int64_t grid = (a.M * ((a.N + 3) / 4) + 255) / 256;
+            hipLaunchKernelGGL((matmul_short_kernel<DT, FORM == FEED_GATED>), dim3((uint32_t)(grid < (1 << 22) ? grid : 1 << 22)), dim3(256), 0, (hipStream_t)stream, a);
+            return hipGetLastError() == hipSuccess ? 0 : 1;
+        }
     const bool q = direct(a.q[0], size, Q_STRIDED), p = direct(a.p[0], size, P_STRIDED) && (!TWO || direct(a.p[1], size, P_STRIDED));
     if constexpr (FORM >= FEED_RIGHT) return p ? launch_shape<DT, FORM, true, true>(a, stream) : launch_shape<DT, FORM, true, false>(a, stream);
     else return q && p ? launch_shape<DT, FORM, true, true>(a, stream) : launch_shape<DT, FORM, false, false>(a, stream);
