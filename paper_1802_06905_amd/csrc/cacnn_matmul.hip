@@ -12,6 +12,14 @@
 //     both operands use the same assignment.
 //   contraction strided ([k][row]): LDS keeps the rows of k as they lie in memory, in blocks of 64 bytes (bf16, read by the
 //     transposing loads) or 128 (fp32, read word by word) that change places with k, for the same reason.
+// (The counter of LDS bank conflicts says 0, and LDS is read a fifth of the time.)
+//
+// What bounds large products is the chip's power and what is left between the matrix instructions: bf16 gated (4096, 4096, 4096), 0.27 TFLOP in 250 us,
+// keeps the matrix pipes busy for 54 % of the cycles at 1.94 GHz; (8192, 4096, 8192) takes 985 us with random data and 786 with zeros.  Measured:
+//     8 bits (8192, 8192, 4096)                       281 us, 1960 TFLOP/s (a library product of 8192 x 8192 x 8192 2670)
+//     bf16 gated (8192, 4096, 8192), three results    1005 us, 1095 TFLOP/s (1410);  its gradients, 8 T C F, 2050 us, 1070 TFLOP/s
+//     fp32 gated (1024, 2048, 2048)                   136 us, 126 TFLOP/s (151)
+// Few rows are bound by the weights' way from memory: one token bf16 (4096, 2 x 8192) 23.5 us on the device, 5.7 TB/s; in 8 bits (4096, 8192) 7.6 us, 4.4 TB/s.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -475,7 +483,7 @@ __global__ void __launch_bounds__(WM* WN * 64, WM* WN == 4 ? 2 : 1) matmul_block
         asm volatile("" ::: "memory");
     };
     // Between two calls of next() the wave multiplies several times, and behind each brings a part of the next slab: all at once, the loads keep it
-    // from issuing products for as long as those of all waves take to be accepted (bf16, 256 x 256: 1012 -> 977 us for 1.1 PFLOP).  With two stages there is one slab only between a load
+    // from issuing products for as long as those of all waves take to be accepted (bf16, 256 x 256: 1012 -> 977 us for 1.1 TFLOP).  With two stages there is one slab only between a load
     // and its wait: early, in one go with four waves, in two with eight (128 x 128 tiles 3 to 20 % slower if spread).
     auto phase_of = [](int phase, int phases) {
         const int n = STAGES > 2 ? phases : WAVES > 4 ? 2 : 1;
@@ -923,7 +931,11 @@ static int launch_shape(const FeedArgs& a, void* stream) {
     if (kernel == MATMUL_WAVES_64_32) return launch_waves<DT, FORM, 2, HALF, QD, PD>(a, stream);
     if constexpr (FORM != FEED_GATED)
         if (kernel == MATMUL_WAVES_64) return launch_waves<DT, FORM, 2, 2, QD, PD>(a, stream);
-    if constexpr (DIRECT)
+    // (two waves to a SIMD where one workgroup has the compute unit: bf16 gated (777, 1008, 1515) 15.3 -> 14.0 us, (512, 2048, 2048) 24.4 -> 23.0; the 8-bit
+    // instructions then have a block of rows each for the columns' operands read from LDS, (1024, 4096, 4096) 32 -> 39)
+    if constexpr (DIRECT && feed_size(DT) > 1)
+        if (kernel == MATMUL_128_DEEP) return launch_block<DT, FORM, 1, 2, 4, 2, 128, 4, QD, PD>(a, stream);
+    if constexpr (DIRECT && feed_size(DT) == 1)
         if (kernel == MATMUL_128_DEEP) return launch_block<DT, FORM, 2, 2, 2, 2, 128, 4, QD, PD>(a, stream);
     if constexpr (DIRECT && DT == FEED_BF16)
         if (kernel == MATMUL_256) return launch_block<DT, FORM, 4, 2, 2, 4, 64, 4, QD, PD>(a, stream);
