@@ -36,13 +36,13 @@ FeedOut output(void* p, int64_t ld, int size) { return {static_cast<char*>(p), l
 int64_t padded(int64_t n) { return (n + 63) / 64 * 64; }      // columns of a row in the workspace
 
 // The workspace of the backward pass: the gradients of gate and up, and, where rows of C elements are no multiple of 16 bytes, X and both weights with rows
-// that are: the products read them two and three times each, and faster straight to LDS (bf16 (2048, 2047, 4095) 490 us in all without the copies, 289 with them).
+// that are: the products read them two and three times each, and faster straight to LDS (bf16 (2048, 2047, 4095) 490 us in all without the copies, 259 with them).
 // Not for few rows, where the copies would be most of the traffic, unless C is too short for a 16-byte load.
 struct Workspace {
     int64_t ld_f, ld_c;            // elements of a row; ld_c 0: no copies
     int64_t grad, x, w;            // bytes of grad_gate (and of grad_up), of the copies of X and of a weight
     Workspace(const cacnn_gated_problem& p, int size)
-        : ld_f(padded(p.F)), ld_c(p.C * size < 16 || (p.C * size % 16 && p.T >= 128) ? padded(p.C) : 0), grad(p.T * ld_f * size), x(p.T * ld_c * size), w(p.F * ld_c * size) {}
+        : ld_f(padded(p.F)), ld_c(p.T > 0 && (p.C * size < 16 || (p.C * size % 16 && p.T >= 128)) ? padded(p.C) : 0), grad(p.T * ld_f * size), x(p.T * ld_c * size), w(p.F * ld_c * size) {}
     int64_t bytes() const { return 2 * grad + x + 2 * w; }
 };
 
@@ -59,7 +59,7 @@ int launched(int rc) { return rc == 0 ? CACNN_OK : CACNN_ERR_LAUNCH; }
 
 // The kernel with the least estimated time.  A workgroup has a compute unit to itself (two of the 128 x 128 tiles with two stages share one), a launch runs in
 // rounds of 256, and a round takes 3 us and what a slab of 128 bytes of the contraction (the dividing waves: four slabs, one each) was measured to take, in us, on
-// shapes of 64 to 8192 rows; operands that come through registers take the dividing waves, which are then one slab ahead only, twice as long:
+// shapes of 64 to 8192 rows; operands that come through registers take the dividing waves twice as long:
 //                                            bf16, 8 bits   fp32 (bound by its matrix instructions)
 //     32 x 32 divided (gated: 32 x 2 x 32)   0.75 (1.15)     0.8 (1.15)
 //     64 x 32 divided (gated: 64 x 2 x 32)   1.15 (1.25)     1.2 (1.9)

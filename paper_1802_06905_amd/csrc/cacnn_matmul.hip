@@ -127,6 +127,7 @@ struct RegisterLoader {
     // slab s of the operand (none if !any: zeros)
     __device__ __forceinline__ void load(int64_t s, bool any, int set) {
         any = any && rows > 0;
+        s = any ? s : 0;                                                          // (a load from there for nothing)
         cut[set] = !any || (STRIDED ? rows < ROWS || (s + 1) * Map::KR > k : (s + 1) * SLAB > k * ESZ);
         const char* const from = base + (STRIDED ? s * Map::KR * ld : 0);
         const int left = (int)min(k - s * Map::KR, (int64_t)Map::KR);             // strided: indices from the slab's first to the operand's last
@@ -525,7 +526,7 @@ __global__ void __launch_bounds__(WM* WN * 64, WM* WN == 4 ? 2 : 1) matmul_block
                 for (int h = 0; h < QB; ++h) multiply<DT>(acc[i][h], pv[set][i], qv[set][h]);
                 __builtin_amdgcn_sched_barrier(0);
                 load_some(phase_of(phase * PB + i, PB * STEPS), phase_of(phase * PB + i + 1, PB * STEPS));
-                    __builtin_amdgcn_sched_barrier(0);
+                __builtin_amdgcn_sched_barrier(0);
             }
         };
         read(0, 0);

@@ -84,7 +84,7 @@ def scaled(torch, rng, rows, cols, block_rows):
 
 PRODUCTS = [  # T, C, K, pad, shift
     (1, 1, 1, 0, 0), (1, 128, 32, 0, 0), (1, 4096, 200, 0, 0), (2, 127, 129, 0, 0), (31, 1000, 65, 0, 0), (33, 256, 1111, 3, 0), (64, 1040, 96, 0, 0),
-    (65, 129, 128, 0, 1), (128, 512, 256, 16, 0), (130, 272, 260, 0, 0), (517, 100, 333, 0, 5), (300, 2048, 384, 0, 0), (700, 384, 640, 0, 16),
+    (65, 129, 128, 0, 1), (128, 512, 256, 16, 0), (130, 272, 260, 0, 0), (517, 100, 333, 0, 5), (300, 2048, 384, 0, 0), (700, 384, 640, 0, 16), (40, 15, 300, 1, 0), (200, 16, 70, 0, 3),
 ]
 
 
@@ -155,6 +155,7 @@ def test_gated_forward_scaled(env, T, C, F, pad, shift, gate):
 SHAPES = [  # T, C, F, pad, shift
     (1, 1, 1, 0, 0), (1, 1024, 96, 0, 0), (2, 7, 65, 0, 0), (17, 512, 128, 0, 0), (32, 1000, 72, 8, 0), (33, 129, 200, 3, 0), (64, 264, 320, 0, 0),
     (65, 64, 33, 0, 1), (129, 255, 130, 0, 0), (256, 512, 256, 0, 8), (300, 1032, 200, 0, 0), (640, 320, 704, 0, 0),
+    (200, 64, 96, 0, 1), (150, 3, 40, 0, 0), (3, 5, 1000, 2, 1),
 ]
 
 
@@ -220,9 +221,9 @@ def test_gradients_that_are_not_wanted(env):
     assert torch.equal(x, x2) and torch.equal(g, g2) and torch.equal(u, u2)
 
 
-def test_no_tokens(env):
+@pytest.mark.parametrize("C,F", [(72, 40), (3, 40)])
+def test_no_tokens(env, C, F):
     cc, torch = env
-    C, F = 72, 40
     empty = lambda n, t=torch.bfloat16: torch.empty((0, n), dtype=t, device="cuda")  # noqa: E731
     w = torch.randn((F, C), device="cuda").bfloat16()
     g, u = torch.full_like(w, 3), torch.full_like(w, 3)
@@ -401,3 +402,35 @@ def test_two_graphs_with_a_workspace_each_run_at_once(env):
         torch.cuda.synchronize()
         for _, _, out, eager, *_ in runs:
             assert all(torch.equal(a, b) for a, b in zip(out, eager))
+
+
+def test_rows_of_two_megabytes(env):
+    """The longest rows, through registers (their first element is not at a multiple of 16 bytes) and straight to LDS; 3 tokens, gradients too."""
+    cc, torch = env
+    T, C, F = 3, 1 << 20, 24
+    print("[feed] rows of 2 MB", flush=True)
+    x, wg, wu = (torch.randn((n, C), device="cuda").mul_(C ** -0.25).bfloat16() for n in (T, F, F))
+    dy = torch.randn((T, F), device="cuda").bfloat16()
+    where = (T, C, F, cc.CACNN_GATE_SILU)
+    results = []
+    for shift in (0, 1):
+        moved = []
+        for t in (x, wg, wu):
+            flat = torch.zeros(t.numel() + 8, dtype=t.dtype, device="cuda")
+            flat[shift:shift + t.numel()].copy_(t.flatten())
+            moved.append(flat[shift:shift + t.numel()].view(t.shape))
+        y, gate, up = (torch.zeros((T, F), dtype=torch.bfloat16, device="cuda") for _ in range(3))
+        cc.cacnn_gated_forward(where, 1, *moved, y, gate=gate, up=up)
+        grads = [torch.zeros_like(t) for t in (x, wg, wu)]
+        work = torch.empty(cc.cacnn_gated_workspace(where, 1), dtype=torch.uint8, device="cuda")
+        cc.cacnn_gated_backward(where, 1, *moved, dy, *grads, work, gate=gate, up=up)
+        results.append((y, gate, up, *grads))
+    for a, b in zip(*results):
+        # the same sums in the same order
+        assert torch.equal(a, b)
+    g = torch.zeros((T, F), dtype=torch.float64, device="cuda")
+    for part in range(0, C, 1 << 16):
+        g += x[:, part:part + (1 << 16)].double() @ wg[:, part:part + (1 << 16)].double().t().contiguous()
+    # C + 1 roundings of the sum of magnitudes, about C * 2 / pi / C^(1/2), and half a step of bf16
+    bound = (C + 1) * 2.0 ** -23 * C ** 0.5 * 0.7 + 2.0 ** -8 * g.abs()
+    assert bool(((results[0][1].double() - g).abs() <= bound).all())
