@@ -31,7 +31,7 @@ bool element_type(int dtype) { return dtype == CACNN_F32 || dtype == CACNN_BF16_
 FeedOperand operand(const void* p, int64_t ld, int size, int64_t rows, int64_t k, bool padded = false) {
     return {static_cast<const char*>(p), ld * size, k, rows, padded};
 }
-FeedOut output(void* p, int64_t ld, int size) { return {static_cast<char*>(p), ld * size, size}; }
+FeedOut output(void* p, int64_t ld, int size) { return {static_cast<char*>(p), ld * size, size, multiple(p, 128) && ld * size % 128 == 0}; }
 
 int64_t padded(int64_t n) { return (n + 63) / 64 * 64; }      // columns of a row in the workspace
 

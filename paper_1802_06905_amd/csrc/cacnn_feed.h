@@ -30,11 +30,12 @@ struct FeedOperand {
     bool padded;     // zeros follow each row's elements up to a multiple of 16 bytes
 };
 
-// An output array of elements of `size` bytes
+// An output array of elements of `size` bytes; lines: its rows start at multiples of a line, 128 bytes
 struct FeedOut {
     char* base;
     int64_t ld;      // bytes
     int32_t size;
+    int32_t lines;
 };
 
 // Which product: the contraction is contiguous in both operands and the columns come in pairs (gated), in both (plain), in the

@@ -16,12 +16,14 @@
 //
 // What bounds large products is the chip's power and what is left between the matrix instructions: bf16 gated (4096, 4096, 4096), 0.27 TFLOP in 250 us,
 // keeps the matrix pipes busy for 54 % of the cycles at 1.94 GHz; (8192, 4096, 8192) takes 985 us with random data and 786 with zeros.  Measured:
-//     8 bits (8192, 8192, 4096)                       281 us, 1960 TFLOP/s (a library product of 8192 x 8192 x 8192 2670)
+//     8 bits (8192, 8192, 4096)                       271 us, 2030 TFLOP/s (a library product of 8192 x 8192 x 8192 2670)
 //     bf16 gated (8192, 4096, 8192), three results    1005 us, 1095 TFLOP/s (1410);  its gradients, 8 T C F, 2050 us, 1070 TFLOP/s
 //     fp32 gated (1024, 2048, 2048)                   136 us, 126 TFLOP/s (151)
 // Few rows are bound by the weights' way from memory: one token bf16 (4096, 2 x 8192) 23.5 us on the device, 5.7 TB/s; in 8 bits (4096, 8192) 7.6 us, 4.4 TB/s.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
+
+#include <type_traits>
 
 #include "cacnn_feed.h"
 #include "cacnn_gate.h"
@@ -299,16 +301,22 @@ __device__ __forceinline__ uint32_t two_bf16(float lo, float hi) {
     return (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)lo) | (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)hi) << 16;
 }
 
-// E adjacent columns from n on of row m, those below `cols`: 16 or 8 bytes
-template <int DT, int E>
+// E adjacent columns from n on of row m, those below `cols`: 16 or 8 bytes.  STREAM: past the L2, for lines that a wave writes whole
+template <int DT, int E, bool STREAM = false>
 __device__ __forceinline__ void store_run(const FeedOut& o, int64_t m, int64_t n, int64_t cols, const float (&v)[E]) {
     constexpr bool WORDS = DT == FEED_F32 || DT == FEED_E4M3_EXACT;
     static_assert(E == 4 || (E == 8 && !WORDS), "what one store takes");
     char* const p = o.base + m * o.ld + n * (WORDS ? 4 : 2);
     if (n + E <= cols) {
-        if constexpr (WORDS) ((MatBytes16*)p)->v = __builtin_bit_cast(mu32x4, mf32x4{v[0], v[1], v[2], v[3]});
-        else if constexpr (E == 4) ((MatBytes8*)p)->v = mu32x2{two_bf16(v[0], v[1]), two_bf16(v[2], v[3])};
-        else ((MatBytes16*)p)->v = mu32x4{two_bf16(v[0], v[1]), two_bf16(v[2], v[3]), two_bf16(v[4], v[5]), two_bf16(v[6], v[7])};
+        if constexpr (!WORDS && E == 4) {
+            ((MatBytes8*)p)->v = mu32x2{two_bf16(v[0], v[1]), two_bf16(v[2], v[3])};
+        } else {
+            mu32x4 x;
+            if constexpr (WORDS) x = __builtin_bit_cast(mu32x4, mf32x4{v[0], v[1], v[2], v[3]});
+            else x = mu32x4{two_bf16(v[0], v[1]), two_bf16(v[2], v[3]), two_bf16(v[4], v[5]), two_bf16(v[6], v[7])};
+            if constexpr (STREAM) __builtin_nontemporal_store(x, (mu32x4*)p);
+            else ((MatBytes16*)p)->v = x;
+        }
     } else {
 #pragma unroll
         for (int e = 0; e < E; ++e)
@@ -320,11 +328,11 @@ __device__ __forceinline__ void store_run(const FeedOut& o, int64_t m, int64_t n
 }
 
 // What becomes of E adjacent columns of a row, given their sums (gated: v of gate, u of up)
-template <int DT, bool GATED, int E>
+template <int DT, bool GATED, bool STREAM, int E>
 __device__ __forceinline__ void finish_run(const FeedArgs& a, int product, int64_t m, int64_t n, const float (&v)[E], const float (&u)[E]) {
     if (m >= a.M) return;
     if constexpr (!GATED) {
-        store_run<DT>(a.out[product], m, n, a.N, v);
+        store_run<DT, E, STREAM>(a.out[product], m, n, a.N, v);
     } else if (feed_size(DT) > 1 && a.grad_out) {
         if (n >= a.grad_cols) return;
         float d[E];
@@ -652,17 +660,24 @@ __global__ void __launch_bounds__(WM* WN * 64, WM* WN == 4 ? 2 : 1) matmul_block
                 *(mf32x4*)(turn + j * PITCH + (i * 32 + v * 2 + g * 4) * 4) = mf32x4{acc[i][h][v], acc[i][h][v + 1], acc[i][h][v + 2], acc[i][h][v + 3]};
         asm volatile("" ::: "memory");
         __builtin_amdgcn_wave_barrier();
+        auto rows = [&](auto stream) MAT_INLINE {
 #pragma unroll 1
-        for (int row = lane / LANES; row < 32; row += 64 / LANES) {
-            const int col = lane % LANES * RUN;
-            float v[RUN], u[RUN];
+            for (int row = lane / LANES; row < 32; row += 64 / LANES) {
+                const int col = lane % LANES * RUN;
+                float v[RUN], u[RUN];
 #pragma unroll
-            for (int e = 0; e < RUN; ++e) {
-                v[e] = *(const float*)(turn + row * PITCH + (col + e) * 4);
-                u[e] = S::GATED ? *(const float*)(turn + row * PITCH + (COLS + col + e) * 4) : 0.f;
+                for (int e = 0; e < RUN; ++e) {
+                    v[e] = *(const float*)(turn + row * PITCH + (col + e) * 4);
+                    u[e] = S::GATED ? *(const float*)(turn + row * PITCH + (COLS + col + e) * 4) : 0.f;
+                }
+                finish_run<DT, S::GATED, decltype(stream)::value>(a, at.product, m0 + (wm * QB + h) * 32 + row, n0 + block_of(0) * 32 + col, v, u);
             }
-            finish_run<DT, S::GATED>(a, at.product, m0 + (wm * QB + h) * 32 + row, n0 + block_of(0) * 32 + col, v, u);
-        }
+        };
+        // (whole lines past the L2: the 8-bit product of (8192, 8192, 4096) 281 -> 271 us.  A gated wave's are half lines: 1015 -> 1042; the gradients in
+        // bf16, four times the arithmetic to a line, gain nothing: 2024 -> 2038)
+        constexpr bool STREAMS = ESZ == 1 && !S::GATED;
+        if (STREAMS && a.out[at.product].lines) rows(std::integral_constant<bool, STREAMS>{});
+        else rows(std::false_type{});
         asm volatile("" ::: "memory");
         __builtin_amdgcn_wave_barrier();
     }
@@ -857,7 +872,7 @@ __global__ void __launch_bounds__(256) matmul_waves_kernel(const FeedArgs a) {
             float v[4], u[4];
             sum(i, h, v);
             sum(S::GATED ? i + PB / 2 : i, h, u);
-            finish_run<DT, S::GATED>(a, at.product, m0 + h * 32 + j, n0 + block_of(i) * 32 + wave * 8 + g * 4, v, u);
+            finish_run<DT, S::GATED, false>(a, at.product, m0 + h * 32 + j, n0 + block_of(i) * 32 + wave * 8 + g * 4, v, u);
         }
 }
 
@@ -884,7 +899,7 @@ __global__ void __launch_bounds__(256) matmul_short_kernel(const FeedArgs a) {
                 if (feed_size(DT) == 1 && n + e < a.N) x *= a.q_scale[m] * a.p_scale[h][(n + e) / kScaleBlock];
                 sum[h][e] = x;
             }
-        finish_run<DT, GATED>(a, 0, m, n, sum[0], sum[GATED ? 1 : 0]);
+        finish_run<DT, GATED, false>(a, 0, m, n, sum[0], sum[GATED ? 1 : 0]);
     }
 }
 
