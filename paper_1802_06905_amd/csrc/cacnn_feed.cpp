@@ -59,21 +59,23 @@ int launched(int rc) { return rc == 0 ? CACNN_OK : CACNN_ERR_LAUNCH; }
 
 // The kernel with the least estimated time.  A workgroup has a compute unit to itself (two of the 128 x 128 tiles with two stages share one), a launch runs in
 // rounds of 256, and a round takes 3 us and what a slab of 128 bytes of the contraction (the dividing waves: four slabs, one each) was measured to take, in us, on
-// shapes of 64 to 8192 rows; operands that come through registers take the dividing waves twice as long:
+// shapes of 64 to 8192 rows; operands that come through registers take the dividing waves 1.7 times as long:
 //                                            bf16, 8 bits   fp32 (bound by its matrix instructions)
 //     32 x 32 divided (gated: 32 x 2 x 32)   0.75 (1.15)     0.8 (1.15)
-//     64 x 32 divided (gated: 64 x 2 x 32)   1.15 (1.25)     1.2 (1.9)
-//     64 x 64 divided                        1.45            1.9
+//     64 x 32 divided (gated: 64 x 2 x 32)   1.15 (1.25)     1.4 (2.15)
+//     64 x 64 divided                        1.45            2.4
 //     128 x 128, four stages                 0.85            2.0
 //     128 x 128, two of two stages           1.6             3.8
 //     256 x 256                              2.0             -
+//     64 x 128, three of two stages          -               1.0 for each tile of a compute unit, 1.3 for one
 // Examples, us, the chosen kernel first: 8 bits (64, 8192, 4096) 15 on 32 x 32, 22 on 64 x 32; (256, 4096, 4096) 15.5 on 64 x 64, 22 on 64 x 32; (1024, 4096, 4096)
 // 34 on 128 x 128 with four stages, 39 with two, 47 on 64 x 64; (2048, 4096, 4096) 51 with two stages, 64 with four, 78 on 256 x 256; bf16 gated (8192, 4096, 8192)
-// 972 on 256 x 256, 1135 on 128 x 128 with two stages.
+// 972 on 256 x 256, 1135 on 128 x 128 with two stages; fp32 gated (1028, 6976, 3712) 874 on 64 x 128, 975 on 64 x 32, 1275 on 128 x 128, (6261, 2494, 912) through
+// registers 522, 630 and 631.
 int cacnn::matmul_kernel(const FeedArgs& a, int form, int dtype, bool direct) {
     const bool f32 = dtype == FEED_F32, gated = form == FEED_GATED;
     const int64_t half = gated ? 2 : 1;
-    const double slabs = (double)a.q[0].k * feed_size(dtype) / 128 * a.segments, ahead = direct ? 1.0 : 2.0;
+    const double slabs = (double)a.q[0].k * feed_size(dtype) / 128 * a.segments, ahead = direct ? 1.0 : 1.7;
     auto us = [&](int64_t rows, int64_t cols, int waves, double slab_us, int64_t at_once = 256) {
         const int64_t tiles = (a.M + rows - 1) / rows * ((a.N + cols - 1) / cols) * a.products;
         return (double)((tiles + at_once - 1) / at_once) * (3.0 + std::ceil(slabs / waves) * slab_us);
@@ -83,10 +85,15 @@ int cacnn::matmul_kernel(const FeedArgs& a, int form, int dtype, bool direct) {
     auto candidate = [&](int kernel, double t) {
         if (t < least) least = t, best = kernel;
     };
-    candidate(MATMUL_WAVES_64_32, us(64, 32, 4, ahead * (gated ? (f32 ? 1.9 : 1.25) : f32 ? 1.2 : 1.15)));
-    if (!gated) candidate(MATMUL_WAVES_64, us(64, 64, 4, ahead * (f32 ? 1.9 : 1.45)));
+    candidate(MATMUL_WAVES_64_32, us(64, 32, 4, ahead * (gated ? (f32 ? 2.15 : 1.25) : f32 ? 1.4 : 1.15)));
+    if (!gated) candidate(MATMUL_WAVES_64, us(64, 64, 4, ahead * (f32 ? 2.4 : 1.45)));
     if (direct) candidate(MATMUL_128_DEEP, us(128, 128 / half, 1, f32 ? 2.0 : 0.85));
     candidate(MATMUL_128, us(128, 128 / half, 1, f32 ? 3.8 : 1.6, 512));
+    if (f32) {
+        // (what a compute unit's tiles take is what their matrix instructions take, however many share it, and for one tile the time from load to LDS)
+        const int64_t cols = 128 / half, tiles = (a.M + 63) / 64 * ((a.N + cols - 1) / cols) * a.products;
+        candidate(MATMUL_64_128, 3.0 + std::ceil(slabs) * std::max(direct ? 1.3 : 1.9, (double)((tiles + 255) / 256)));
+    }
     if (direct && (dtype == FEED_BF16 || dtype == FEED_E4M3)) candidate(MATMUL_256, us(256, 256 / half, 1, 2.0));
     return best;
 }

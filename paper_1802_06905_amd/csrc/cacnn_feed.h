@@ -65,8 +65,8 @@ struct FeedArgs {
 };
 
 // The kernels of a product: workgroups whose four waves divide the contraction, with 32 x 32, 64 x 32 and 64 x 64 of the sums (gated: half as many columns of
-// Out), and workgroups with 128 x 128 (four stages in LDS, or two and two workgroups to a compute unit) and 256 x 256
-enum { MATMUL_WAVES_32 = 0, MATMUL_WAVES_64_32 = 1, MATMUL_WAVES_64 = 2, MATMUL_128_DEEP = 3, MATMUL_128 = 4, MATMUL_256 = 5 };
+// Out), and workgroups with 128 x 128 (four stages in LDS, or two and two workgroups to a compute unit), 256 x 256, and (fp32) 64 x 128, three to a compute unit
+enum { MATMUL_WAVES_32 = 0, MATMUL_WAVES_64_32 = 1, MATMUL_WAVES_64 = 2, MATMUL_128_DEEP = 3, MATMUL_128 = 4, MATMUL_256 = 5, MATMUL_64_128 = 6 };
 // Which of them takes the product of operands that go straight to LDS or (direct false) through registers
 int matmul_kernel(const FeedArgs& a, int form, int dtype, bool direct);
 

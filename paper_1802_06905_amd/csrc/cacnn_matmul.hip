@@ -957,6 +957,8 @@ static int launch_shape(const FeedArgs& a, void* stream) {
         if (kernel == MATMUL_256) return launch_block<DT, FORM, 4, 2, 2, 4, 64, 4, QD, PD>(a, stream);
     if constexpr (DIRECT && DT == FEED_E4M3)
         if (kernel == MATMUL_256) return launch_block<DT, FORM, 4, 2, 2, 4, 128, 2, QD, PD>(a, stream);
+    if constexpr (DT == FEED_F32)
+        if (kernel == MATMUL_64_128) return launch_block<DT, FORM, 1, 2, 2, 2, 128, 2, QD, PD>(a, stream);
     return launch_block<DT, FORM, 2, 2, 2, 2, 128, 2, QD, PD>(a, stream);
 }
 template <int DT, int FORM>

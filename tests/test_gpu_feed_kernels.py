@@ -11,7 +11,7 @@ from tests.feed_util import Result, put, rounded, within
 pytestmark = pytest.mark.gpu
 
 GATED, PLAIN, RIGHT, BOTH = 0, 1, 2, 3                    # forms, and kernels, as the library numbers them
-W32, W64_32, W64, DEEP, MIDDLE, LARGE = range(6)
+W32, W64_32, W64, DEEP, MIDDLE, LARGE, SMALL = range(7)
 TYPES = {"f32": 0, "bf16": 1, "e4m3": 2, "e4m3 exact": 3}
 
 
@@ -56,13 +56,13 @@ SHAPES = {
     (PLAIN, "e4m3"): [(W32, 26, 672, 126), (W64_32, 465, 688, 547), (W64, 522, 656, 908), (DEEP, 1369, 672, 717), (MIDDLE, 2185, 656, 1796), (LARGE, 2325, 640, 3374)],
     (PLAIN, "e4m3 exact"): [(W32, 120, 656, 61), (W64_32, 633, 656, 392), (W64, 653, 640, 746), (DEEP, 1223, 640, 810), (MIDDLE, 1576, 640, 2496)],
     (GATED, "bf16"): [(W32, 75, 360, 84), (W64_32, 556, 360, 462), (DEEP, 732, 320, 700), (MIDDLE, 1154, 320, 1641), (LARGE, 2325, 320, 1675)],
-    (GATED, "f32"): [(W32, 40, 184, 83), (W64_32, 420, 184, 617), (DEEP, 537, 160, 1055), (MIDDLE, 1626, 160, 1220)],
+    (GATED, "f32"): [(W32, 40, 184, 83), (W64_32, 420, 184, 617), (SMALL, 537, 160, 1055), (DEEP, 918, 176, 1135), (MIDDLE, 1685, 160, 1831)],
     (GATED, "e4m3"): [(W32, 28, 720, 99), (W64_32, 590, 640, 423), (DEEP, 710, 640, 705), (MIDDLE, 1548, 640, 1230), (LARGE, 1288, 656, 2973)],
     (GATED, "e4m3 exact"): [(W32, 24, 688, 66), (W64_32, 388, 640, 703), (DEEP, 800, 640, 609), (MIDDLE, 1424, 656, 1365)],
     (RIGHT, "bf16"): [(W32, 30, 192, 325), (W64_32, 408, 616, 324), (W64, 771, 616, 352), (DEEP, 1221, 856, 330), (MIDDLE, 2492, 1600, 327), (LARGE, 4176, 1968, 329)],
-    (RIGHT, "f32"): [(W32, 42, 120, 214), (W64_32, 466, 624, 162), (W64, 589, 832, 168), (DEEP, 1617, 1256, 168), (MIDDLE, 2478, 1680, 205)],
+    (RIGHT, "f32"): [(W32, 42, 120, 214), (W64_32, 466, 624, 162), (W64, 589, 832, 168), (SMALL, 1216, 856, 162), (DEEP, 1250, 1632, 167), (MIDDLE, 3295, 1840, 166)],
     (BOTH, "bf16"): [(W32, 331, 64, 44), (W64_32, 355, 360, 363), (W64, 328, 528, 542), (DEEP, 326, 560, 911), (MIDDLE, 320, 1184, 1596), (LARGE, 320, 1720, 2309)],
-    (BOTH, "f32"): [(W32, 202, 64, 65), (W64_32, 213, 376, 401), (W64, 186, 408, 577), (DEEP, 167, 824, 1258), (MIDDLE, 162, 784, 2313)],
+    (BOTH, "f32"): [(W32, 202, 64, 65), (W64_32, 213, 376, 401), (W64, 186, 408, 577), (SMALL, 161, 664, 716), (DEEP, 168, 688, 1354), (MIDDLE, 176, 1416, 2062)],
 }
 
 
@@ -125,6 +125,29 @@ def test_gradients(env, form, dtype, kernel, T, C, F):
     expect = feed.gated_backward(x, wg, wu, dy, "silu", feed.HALF_STEP[dtype])
     for name, r in (("grad_x", gx), ("grad_w_gate", gg), ("grad_w_up", gu)):
         within(name, r.numpy(), *expect[name])
+        r.check()
+
+
+def test_64_by_128_tiles_through_registers(env):
+    """Odd sizes in fp32 that take these tiles in both directions, on operands whose rows allow no load to LDS."""
+    cc, torch = env
+    T, C, F = 1267, 803, 625
+    assert [kernel_of(cc, form, "f32", *sizes, False) for form, sizes in ((GATED, (T, F, C)), (RIGHT, (T, C, F)), (BOTH, (F, C, T)))] == [SMALL] * 3
+    say("[feed] 64 x 128 tiles through registers", T, C, F)
+    rng = np.random.default_rng(64)
+    (x, tx), (wg, tg), (wu, tu) = normal(torch, rng, "f32", T, C), normal(torch, rng, "f32", F, C, C ** -0.5), normal(torch, rng, "f32", F, C, C ** -0.5)
+    dy, td = normal(torch, rng, "f32", T, F, 1e-2)
+    y, gx, gg, gu = (Result(torch, rows, cols, torch.float32) for rows, cols in ((T, F), (T, C), (F, C), (F, C)))
+    where = (T, C, F, cc.CACNN_GATE_SILU)
+    tx, tg, tu, td = (a.cuda() for a in (tx, tg, tu, td))
+    cc.cacnn_gated_forward(where, 0, tx, tg, tu, y.view)
+    workspace = torch.empty(cc.cacnn_gated_workspace(where, 0), dtype=torch.uint8, device="cuda")
+    cc.cacnn_gated_backward(where, 0, tx, tg, tu, td, gx.view, gg.view, gu.view, workspace)
+    within("out", y.numpy(), *feed.gated(x, wg, wu, "silu", feed.HALF_STEP["f32"])["out"])
+    expect = feed.gated_backward(x, wg, wu, dy, "silu", feed.HALF_STEP["f32"])
+    for name, r in (("grad_x", gx), ("grad_w_gate", gg), ("grad_w_up", gu)):
+        within(name, r.numpy(), *expect[name])
+    for r in (y, gx, gg, gu):
         r.check()
 
 

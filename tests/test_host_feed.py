@@ -181,7 +181,7 @@ def test_more_that_does_not_fit(calls):
 
 
 # ---- which kernel a product runs on
-W32, W64_32, W64, DEEP, MIDDLE, LARGE = range(6)
+W32, W64_32, W64, DEEP, MIDDLE, LARGE, SMALL = range(7)
 
 
 def kernel(form, dtype, M, N, k, direct=1):
@@ -199,10 +199,12 @@ def test_a_kernel_for_every_size():
             for M in (1, 7, 100, 1000, 10000, (1 << 31) - 1):
                 for N in (1, 100, 5000, 1 << 20):
                     for k in (0, 1, 100, 10000):
-                        assert kernel(form, dtype, M, N, k, 0) in ((W32, W64_32, MIDDLE) if form == 0 else (W32, W64_32, W64, MIDDLE))
-                        chosen = kernel(form, dtype, M, N, k)
-                        assert chosen != LARGE or dtype in (1, 2)
-                        assert form != 0 or chosen != W64
+                        for direct in (0, 1):
+                            chosen = kernel(form, dtype, M, N, k, direct)
+                            assert chosen not in (DEEP, LARGE) or direct
+                            assert chosen != LARGE or dtype in (1, 2)
+                            assert chosen != SMALL or dtype == 0
+                            assert form != 0 or chosen != W64
 
 
 def test_the_module_leaves_what_is_not_usual():
