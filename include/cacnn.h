@@ -273,8 +273,8 @@ int cacnn_pool_forward(const cacnn_problem* problem, int dtype, int mode, const 
  * Arrays are row-major, the last index contiguous:  X [T][C] of T tokens with C channels, weights [K][C] or [F][C] (a Filter with R = S = 1),
  * results [T][K] or [T][F].  Each array's rows may lie further apart than their length: ld_* is the distance in elements, 0 for rows that follow one
  * another.  T may be 0 (nothing is written but weight gradients, which are zeros; pointers to arrays of T rows may then be NULL).
- * Limits: T <= 2^31 - 1, row lengths and strides <= 2^20, (rows / 128) times (columns / 64) of a result < 2^24 (1.3e11 elements; of both
- * weights' gradients together).
+ * Limits: T <= 2^31 - 1, row lengths and strides <= 2^20, rows / 128 times columns / 64 of a result, each rounded up, < 2^24 (1.3e11 elements).
+ * For a gated projection those of X's gradient and of both weights' together too, whichever results a call asks for.
  * Pointers must be aligned to their element size; results must not overlap operands.  Accumulation is in fp32; a result in bf16 is rounded once,
  * to nearest even.  Every call adds up in a fixed order: the same call gives the same bits.  Calls enqueue on the stream and return; they never
  * synchronise, allocate nothing, keep no reference and may be captured into a graph.

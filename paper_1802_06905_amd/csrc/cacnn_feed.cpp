@@ -15,7 +15,8 @@ namespace {
 
 // Row lengths and strides: 32-bit offsets within the 256 rows of a tile, in units of a byte, stay below 2^30
 constexpr int64_t kMostColumns = 1 << 20, kMostRows = INT32_MAX;
-// and the threads of a launch below 2^32: 256 for each 128 x 64 of a gated projection's result
+// and the threads of a launch below 2^32 on the 128 x 128 tiles, 256 for each 128 x 64 of a gated projection's result (other kernels are not chosen where
+// they would need more)
 bool tiles_in_range(int64_t rows, int64_t cols) { return (rows + 127) / 128 * ((cols + 63) / 64) < (1 << 24); }
 
 bool columns(int64_t n) { return n >= 1 && n <= kMostColumns; }
@@ -74,27 +75,28 @@ int launched(int rc) { return rc == 0 ? CACNN_OK : CACNN_ERR_LAUNCH; }
 // registers 522, 630 and 631.
 int cacnn::matmul_kernel(const FeedArgs& a, int form, int dtype, bool direct) {
     const bool f32 = dtype == FEED_F32, gated = form == FEED_GATED;
-    const int64_t half = gated ? 2 : 1;
     const double slabs = (double)a.q[0].k * feed_size(dtype) / 128 * a.segments, ahead = direct ? 1.0 : 1.7;
-    auto us = [&](int64_t rows, int64_t cols, int waves, double slab_us, int64_t at_once = 256) {
-        const int64_t tiles = (a.M + rows - 1) / rows * ((a.N + cols - 1) / cols) * a.products;
-        return (double)((tiles + at_once - 1) / at_once) * (3.0 + std::ceil(slabs / waves) * slab_us);
+    auto tiles = [&](const MatmulTile& t, int64_t cols) { return (a.M + t.rows - 1) / t.rows * ((cols + t.cols - 1) / t.cols) * a.products; };
+    // (the 128 x 128 tiles take whatever the entry points let through)
+    int best = MATMUL_128;
+    double least = INFINITY;
+    auto candidate = [&](int kernel, double us) {
+        const MatmulTile t = matmul_tile(kernel, form, dtype);
+        // the runtime launches less than 2^32 threads
+        if (us < least && tiles(t, gated && a.grad_out ? a.grad_cols : a.N) * t.threads < (1ll << 32)) least = us, best = kernel;
     };
-    int best = MATMUL_WAVES_32;
-    double least = us(32, 32, 4, ahead * (gated ? 1.15 : f32 ? 0.8 : 0.75));
-    auto candidate = [&](int kernel, double t) {
-        if (t < least) least = t, best = kernel;
+    auto rounds = [&](int kernel, int waves, double slab_us, int64_t at_once = 256) {
+        candidate(kernel, (double)((tiles(matmul_tile(kernel, form, dtype), a.N) + at_once - 1) / at_once) * (3.0 + std::ceil(slabs / waves) * slab_us));
     };
-    candidate(MATMUL_WAVES_64_32, us(64, 32, 4, ahead * (gated ? (f32 ? 2.15 : 1.25) : f32 ? 1.4 : 1.15)));
-    if (!gated) candidate(MATMUL_WAVES_64, us(64, 64, 4, ahead * (f32 ? 2.4 : 1.45)));
-    if (direct) candidate(MATMUL_128_DEEP, us(128, 128 / half, 1, f32 ? 2.0 : 0.85));
-    candidate(MATMUL_128, us(128, 128 / half, 1, f32 ? 3.8 : 1.6, 512));
-    if (f32) {
-        // (what a compute unit's tiles take is what their matrix instructions take, however many share it, and for one tile the time from load to LDS)
-        const int64_t cols = 128 / half, tiles = (a.M + 63) / 64 * ((a.N + cols - 1) / cols) * a.products;
-        candidate(MATMUL_64_128, 3.0 + std::ceil(slabs) * std::max(direct ? 1.3 : 1.9, (double)((tiles + 255) / 256)));
-    }
-    if (direct && (dtype == FEED_BF16 || dtype == FEED_E4M3)) candidate(MATMUL_256, us(256, 256 / half, 1, 2.0));
+    rounds(MATMUL_WAVES_32, 4, ahead * (gated ? 1.15 : f32 ? 0.8 : 0.75));
+    rounds(MATMUL_WAVES_64_32, 4, ahead * (gated ? (f32 ? 2.15 : 1.25) : f32 ? 1.4 : 1.15));
+    if (!gated) rounds(MATMUL_WAVES_64, 4, ahead * (f32 ? 2.4 : 1.45));
+    if (direct) rounds(MATMUL_128_DEEP, 1, f32 ? 2.0 : 0.85);
+    rounds(MATMUL_128, 1, f32 ? 3.8 : 1.6, 512);
+    // (what a compute unit's tiles take is what their matrix instructions take, however many share it, and for one tile the time from load to LDS)
+    if (f32)
+        candidate(MATMUL_64_128, 3.0 + std::ceil(slabs) * std::max(direct ? 1.3 : 1.9, (double)((tiles(matmul_tile(MATMUL_64_128, form, dtype), a.N) + 255) / 256)));
+    if (direct && (dtype == FEED_BF16 || dtype == FEED_E4M3)) rounds(MATMUL_256, 1, 2.0);
     return best;
 }
 

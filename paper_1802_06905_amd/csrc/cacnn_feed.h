@@ -67,6 +67,22 @@ struct FeedArgs {
 // The kernels of a product: workgroups whose four waves divide the contraction, with 32 x 32, 64 x 32 and 64 x 64 of the sums (gated: half as many columns of
 // Out), and workgroups with 128 x 128 (four stages in LDS, or two and two workgroups to a compute unit), 256 x 256, and (fp32) 64 x 128, three to a compute unit
 enum { MATMUL_WAVES_32 = 0, MATMUL_WAVES_64_32 = 1, MATMUL_WAVES_64 = 2, MATMUL_128_DEEP = 3, MATMUL_128 = 4, MATMUL_256 = 5, MATMUL_64_128 = 6 };
+// What one workgroup of a kernel owns of Out, and its threads
+struct MatmulTile {
+    int rows, cols, threads;
+};
+constexpr MatmulTile matmul_tile(int kernel, int form, int dtype) {
+    const int half = form == FEED_GATED ? 2 : 1;
+    switch (kernel) {
+        case MATMUL_WAVES_32: return {32, 32, 256};
+        case MATMUL_WAVES_64_32: return {64, 32, 256};
+        case MATMUL_WAVES_64: return {64, 64, 256};
+        case MATMUL_128_DEEP: return {128, 128 / half, feed_size(dtype) > 1 ? 512 : 256};
+        case MATMUL_256: return {256, 256 / half, 512};
+        case MATMUL_64_128: return {64, 128 / half, 256};
+        default: return {128, 128 / half, 256};
+    }
+}
 // Which of them takes the product of operands that go straight to LDS or (direct false) through registers
 int matmul_kernel(const FeedArgs& a, int form, int dtype, bool direct);
 

@@ -922,14 +922,21 @@ static int launch_tiles(void (*kernel)(const FeedArgs), OncePerDevice& once, Fee
     hipLaunchKernelGGL(kernel, dim3(a.n_tiles), dim3(threads), S::LDS, (hipStream_t)stream, a);
     return hipGetLastError() == hipSuccess ? 0 : 1;
 }
-template <int DT, int FORM, int QB, int PB, int WM, int WN, int SLAB, int STAGES, bool QD, bool PD>
+// Whether kernel KERNEL's workgroups are what its choice takes them for
+template <int KERNEL, int DT, int FORM, class S>
+constexpr bool as_chosen(int threads) {
+    return matmul_tile(KERNEL, FORM, DT).rows == S::BM && matmul_tile(KERNEL, FORM, DT).cols == S::COLS && matmul_tile(KERNEL, FORM, DT).threads == threads;
+}
+template <int KERNEL, int DT, int FORM, int QB, int PB, int WM, int WN, int SLAB, int STAGES, bool QD, bool PD>
 static int launch_block(const FeedArgs& a, void* stream) {
+    static_assert(as_chosen<KERNEL, DT, FORM, BlockShape<DT, FORM, QB, PB, WM, WN, SLAB, STAGES>>(WM * WN * 64), "the tile in cacnn_feed.h");
     static OncePerDevice once;
     return launch_tiles<BlockShape<DT, FORM, QB, PB, WM, WN, SLAB, STAGES>>(matmul_block_kernel<DT, FORM, QB, PB, WM, WN, SLAB, STAGES, QD, PD>, once, a,
                                                                             WM * WN * 64, stream);
 }
-template <int DT, int FORM, int QB, int PB, bool QD, bool PD>
+template <int KERNEL, int DT, int FORM, int QB, int PB, bool QD, bool PD>
 static int launch_waves(const FeedArgs& a, void* stream) {
+    static_assert(as_chosen<KERNEL, DT, FORM, WaveShape<DT, FORM, QB, PB>>(256), "the tile in cacnn_feed.h");
     static OncePerDevice once;
     return launch_tiles<WaveShape<DT, FORM, QB, PB>>(matmul_waves_kernel<DT, FORM, QB, PB, QD, PD>, once, a, 256, stream);
 }
@@ -943,23 +950,23 @@ static int launch_shape(const FeedArgs& a, void* stream) {
     constexpr bool DIRECT = QD && PD;
     constexpr int HALF = FORM == FEED_GATED ? 2 : 1;
     const int kernel = matmul_kernel(a, FORM, DT, DIRECT);
-    if (kernel == MATMUL_WAVES_32) return launch_waves<DT, FORM, 1, HALF, QD, PD>(a, stream);
-    if (kernel == MATMUL_WAVES_64_32) return launch_waves<DT, FORM, 2, HALF, QD, PD>(a, stream);
+    if (kernel == MATMUL_WAVES_32) return launch_waves<MATMUL_WAVES_32, DT, FORM, 1, HALF, QD, PD>(a, stream);
+    if (kernel == MATMUL_WAVES_64_32) return launch_waves<MATMUL_WAVES_64_32, DT, FORM, 2, HALF, QD, PD>(a, stream);
     if constexpr (FORM != FEED_GATED)
-        if (kernel == MATMUL_WAVES_64) return launch_waves<DT, FORM, 2, 2, QD, PD>(a, stream);
+        if (kernel == MATMUL_WAVES_64) return launch_waves<MATMUL_WAVES_64, DT, FORM, 2, 2, QD, PD>(a, stream);
     // (two waves to a SIMD where one workgroup has the compute unit: bf16 gated (777, 1008, 1515) 15.3 -> 14.0 us, (512, 2048, 2048) 24.4 -> 23.0; the 8-bit
     // instructions then have a block of rows each for the columns' operands read from LDS, (1024, 4096, 4096) 32 -> 39)
     if constexpr (DIRECT && feed_size(DT) > 1)
-        if (kernel == MATMUL_128_DEEP) return launch_block<DT, FORM, 1, 2, 4, 2, 128, 4, QD, PD>(a, stream);
+        if (kernel == MATMUL_128_DEEP) return launch_block<MATMUL_128_DEEP, DT, FORM, 1, 2, 4, 2, 128, 4, QD, PD>(a, stream);
     if constexpr (DIRECT && feed_size(DT) == 1)
-        if (kernel == MATMUL_128_DEEP) return launch_block<DT, FORM, 2, 2, 2, 2, 128, 4, QD, PD>(a, stream);
+        if (kernel == MATMUL_128_DEEP) return launch_block<MATMUL_128_DEEP, DT, FORM, 2, 2, 2, 2, 128, 4, QD, PD>(a, stream);
     if constexpr (DIRECT && DT == FEED_BF16)
-        if (kernel == MATMUL_256) return launch_block<DT, FORM, 4, 2, 2, 4, 64, 4, QD, PD>(a, stream);
+        if (kernel == MATMUL_256) return launch_block<MATMUL_256, DT, FORM, 4, 2, 2, 4, 64, 4, QD, PD>(a, stream);
     if constexpr (DIRECT && DT == FEED_E4M3)
-        if (kernel == MATMUL_256) return launch_block<DT, FORM, 4, 2, 2, 4, 128, 2, QD, PD>(a, stream);
+        if (kernel == MATMUL_256) return launch_block<MATMUL_256, DT, FORM, 4, 2, 2, 4, 128, 2, QD, PD>(a, stream);
     if constexpr (DT == FEED_F32)
-        if (kernel == MATMUL_64_128) return launch_block<DT, FORM, 1, 2, 2, 2, 128, 2, QD, PD>(a, stream);
-    return launch_block<DT, FORM, 2, 2, 2, 2, 128, 2, QD, PD>(a, stream);
+        if (kernel == MATMUL_64_128) return launch_block<MATMUL_64_128, DT, FORM, 1, 2, 2, 2, 128, 2, QD, PD>(a, stream);
+    return launch_block<MATMUL_128, DT, FORM, 2, 2, 2, 2, 128, 2, QD, PD>(a, stream);
 }
 template <int DT, int FORM>
 static int launch_form(const FeedArgs& a, void* stream) {
