@@ -100,6 +100,34 @@ def activation(name, g):
     return 0.5 * g * (1 + t), 0.5 * (1 + t) + 0.5 * g * (1 - t * t) * k * (1 + 3 * 0.044715 * g * g), 0.9
 
 
+_erfc = np.vectorize(math.erfc, otypes=[float])
+
+
+def activation_steps(name, g):
+    """(act, how far its 32-bit steps may be, act', how far its may be), relative to the numbers that they multiply and add, so that a gate far below
+    zero, whose act is small, has to be right in its leading digits too.  Counted: 2^-24 for a rounding or a constant's, an ulp for a power of two or a
+    reciprocal, 16 for the complementary error function, and what a relative error r of its argument y makes of e^y: |y| r."""
+    ulp, tiny = 2.0 ** -23, 2.0 ** -120
+    if name == "gelu":
+        share = 0.5 * _erfc(-g / math.sqrt(2))
+        # d ln erfc(z) / d ln z is at most 2 z^2 + 1 in magnitude, z = x / sqrt 2 of two roundings
+        off = share * (16 + g * g + 2) * ulp
+        rest, rest_off = g * np.exp(-g * g / 2) / math.sqrt(2 * math.pi), (0.75 * g * g + 4) * ulp
+    else:
+        # share = 1 / (1 + e^-y)
+        k = math.sqrt(8 / math.pi)
+        y = g if name == "silu" else k * g * (1 + 0.044715 * g * g)
+        bend = np.ones_like(g) if name == "silu" else k * (1 + 0.134145 * g * g)
+        share = np.where(y < 0, np.exp(-np.abs(y)), 1.0) / (1 + np.exp(-np.abs(y)))
+        other = np.where(y > 0, np.exp(-np.abs(y)), 1.0) / (1 + np.exp(-np.abs(y)))
+        # y is of two roundings (with the constant that turns e into 2) or of nine, and counts by 1 - share
+        off = share * ((1 if name == "silu" else 5) * np.abs(y) * other + 4) * ulp
+        rest = g * share * other * bend
+        rest_off = np.abs(rest) * 5 * ulp + np.abs(g) * bend * (off * np.abs(other - share) + share * ulp)
+        return g * share, np.abs(g) * off + ulp * np.abs(g * share) + tiny, share + rest, off + rest_off + ulp * np.abs(share + rest) + tiny
+    return g * share, np.abs(g) * off + ulp * np.abs(g * share) + tiny, share + rest, off + np.abs(rest) * rest_off + ulp * np.abs(share + rest) + tiny
+
+
 def _off(g):
     """How far the activation's 32-bit steps may be, of 1 + |g|: a power of two of an argument that grows with g, a reciprocal, a few products."""
     return 2.0 ** -20 * (1 + np.abs(g)) ** 2

@@ -8,7 +8,8 @@ namespace cacnn {
 
 enum { GATE_SILU = 0, GATE_GELU = 1, GATE_GELU_TANH = 2 };
 
-// 1 / (1 + e^-x) from the hardware's power of two and reciprocal, each within an ulp: 0 where e^-x overflows, 1 where it vanishes
+// 1 / (1 + e^-x) from the hardware's power of two and reciprocal, each within an ulp: 0 where it is below 2^-126 (x < -87.3; the reciprocal has no
+// subnormal results), 1 where e^-x vanishes
 __device__ __forceinline__ float gate_sigmoid(float x) {
     return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(x * -1.44269504088896f));
 }
@@ -16,9 +17,12 @@ __device__ __forceinline__ float gate_sigmoid(float x) {
 // 0.5 (1 + tanh y) = sigmoid(2 y), y = sqrt(2 / pi) (x + 0.044715 x^3)
 __device__ __forceinline__ float gate_tanh_share(float x) { return gate_sigmoid(1.59576912160573f * x * (1.f + 0.044715f * x * x)); }
 
+// Phi(x), the normal distribution's integral, from the complement: 1 + erf(x / sqrt 2) cancels for negative gates, 4 % off at -5 and nothing at -5.5
+__device__ __forceinline__ float gate_normal_share(float x) { return 0.5f * erfcf(x * -0.70710678118655f); }
+
 __device__ __forceinline__ float gate_value(int activation, float x) {
     if (activation == GATE_SILU) return x * gate_sigmoid(x);
-    if (activation == GATE_GELU) return x * (0.5f + 0.5f * erff(x * 0.70710678118655f));
+    if (activation == GATE_GELU) return x * gate_normal_share(x);
     return x * gate_tanh_share(x);
 }
 
@@ -29,7 +33,7 @@ __device__ __forceinline__ void gate_grad(int activation, float x, float up, flo
         share = gate_sigmoid(x);
         slope = x * (share * (1.f - share));
     } else if (activation == GATE_GELU) {
-        share = 0.5f + 0.5f * erff(x * 0.70710678118655f);
+        share = gate_normal_share(x);
         slope = x * (0.398942280401433f * __builtin_amdgcn_exp2f(x * x * -0.72134752044448f));
     } else {
         share = gate_tanh_share(x);
