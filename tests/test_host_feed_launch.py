@@ -70,3 +70,56 @@ for _ in range(4000):
         taken += rc == OK
 assert taken > 8000, taken
 ''')
+
+
+PRODUCTS = r'''
+def product(symbol):
+    """The product's kernel that a symbol belongs to, with its template's arguments, or None."""
+    m = re.search(r"matmul_(block|waves|short)_kernelI((?:L[ib]\d+E)+)", symbol)
+    return m and m.group(1) + " " + ",".join(re.findall(r"L[ib](\d+)E", m.group(2)))
+def launched(rc):
+    assert rc == OK, rc
+    return {product(k) for k in kernels()} - {None}
+def listed(call, dtype, T, C, F, pad, shift):
+    code, size = int(dtype == "bf16"), 1 if call in ("matmul", "scaled") else 2 if dtype == "bf16" else 4
+    at = A + shift * size
+    if call == "matmul": return launched(matmul(T, C, F, code, (C + pad, 0, 0), at))
+    if call == "scaled": return launched(scaled(T, C, F, code, 0, (C + pad, 0, 0, 0, 0, 0), at))
+    if call == "forward": return launched(forward(T, C, F, code, 0, (C + pad, 0, 0, 0, 0, 0), at))
+    return launched(backward(T, C, F, code, True, 0, (C + pad, C + pad, 0, 0, C + pad, C + pad), at, at, at))
+'''
+
+
+def test_every_product_kernel_is_tested(run):
+    """The calls listed for the kernels that bring operands through registers launch them, and those kernels, and the ones that the other tests on a GPU launch, are all
+    that calls of many sizes, addresses and strides launch."""
+    from tests import feed_shapes, test_gpu_feed, test_gpu_feed_kernels
+    run(PRODUCTS + f"rows = {feed_shapes.THROUGH_REGISTERS!r}\nshapes = {test_gpu_feed_kernels.SHAPES!r}\nsmall = {test_gpu_feed.PRODUCTS + test_gpu_feed.SHAPES!r}\n" + r'''
+tested = set()
+for kernel, *call in rows:
+    names = listed(*call)
+    assert kernel in names and kernel.split(",")[-1] == "0", (kernel, call, names)
+    tested.add(kernel)
+for (form, dtype), all_ in shapes.items():
+    for _, T, C, F in all_:
+        if form == 1: tested |= listed("matmul", "bf16" if dtype == "e4m3" else "f32", T, C, F, 0, 0)
+        elif dtype.startswith("e4m3"): tested |= listed("scaled", "bf16" if dtype == "e4m3" else "f32", T, C, F, 0, 0)
+        else: tested |= listed("forward" if form == 0 else "backward", dtype, T, C, F, 0, 0)
+for T, C, F, pad, shift in small:
+    for dtype in ("f32", "bf16"):
+        for call in ("matmul", "scaled", "forward"):
+            tested |= listed(call, dtype, T, C, F, pad, shift)
+rng = random.Random(5)
+def size(high):
+    n, kind = int(2 ** rng.uniform(0, high)), rng.random()
+    return max(1, n if kind < 0.4 else n // 16 * 16 if kind < 0.7 else n // 128 * 128)
+reached = set()
+for _ in range(20000):
+    T, C, F, dtype, pad = size(14), size(13.5), size(14), rng.randint(0, 1), int(rng.random() < 0.3)
+    x, w = A + 4 * (rng.random() < 0.4), A + 4 * (rng.random() < 0.4)
+    ld, ld_w = C + pad, C + pad * (rng.random() < 0.5)
+    for rc in (matmul(T, C, F, dtype, (ld, 0, 0), x), scaled(T, C, F, dtype, 0, (ld, 0, 0, 0, 0, 0), x), forward(T, C, F, dtype, 0, (ld, 0, 0, 0, 0, 0), x),
+               backward(T, C, F, dtype, rng.random() < 0.5, 0, (ld, ld_w, 0, 0, 0, 0), x, w, w)):
+        reached |= launched(rc)
+assert len(reached) > 90 and reached <= tested, sorted(reached - tested)
+''')
