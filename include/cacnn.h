@@ -308,7 +308,9 @@ typedef struct {
 
 /*
  * Out[t][k] = sum over blocks b of x_scale[t][b] w_scale[k / 128][b] * (sum over c in block b of X[t][c] W[k][c]), X and W in 8-bit floats.
- * Products are exact; each block's sum is multiplied by fp32's product of its two scales and added in fp32.  Scales may be any fp32.
+ * Products are exact; each block's sum is multiplied by fp32's product of its two scales and added in fp32.  Scales may be any fp32, and their product
+ * is what fp32 makes of it: infinite where it overflows (with a sum of 0: NaN), subnormal or 0, with what that rounds off, below 2^-126.
+ * (The powers of two that cacnn_quantize gives multiply exactly down to 2^-149.)
  * An fp32 result's sums are held in fp32 throughout.  A bf16 result comes from the 8-bit matrix instructions, twice as fast, which add eight
  * neighbouring products with what lies more than 13 bits below the largest's leading bit cut off: at most 7 * 2^-13 of each eight's largest product,
  * about 1e-4 of a sum of random products, a twentieth of the rounding to bf16.
