@@ -37,8 +37,13 @@ FeedOut output(void* p, int64_t ld, int size) { return {static_cast<char*>(p), l
 int64_t padded(int64_t n) { return (n + 63) / 64 * 64; }      // columns of a row in the workspace
 
 // The workspace of the backward pass: the gradients of gate and up, and, where rows of C elements are no multiple of 16 bytes, X and both weights with rows
-// that are: the products read them two and three times each, and faster straight to LDS (bf16 (2048, 2047, 4095) 490 us in all without the copies, 259 with them).
-// Not for few rows, where the copies would be most of the traffic, unless C is too short for a 16-byte load.
+// that are: the products read them two and three times each, and faster straight to LDS.  Not for few rows, where the copies would be most of the traffic, unless C is
+// too short for a 16-byte load.  us in all, without copies and with them, gate and up kept | computed again:
+//     T                      64                       128                      256                      2048
+//     bf16 (T, 4095, 4095)   69 : 75 | 85 : 85        77 : 82 | 101 : 95       101 : 94 | 152 : 121     414 : 320 | 597 : 428
+//     bf16 (T, 1001, 1515)   25.5 : 26.6 | 32 : 31    27.2 : 27.2 | 34 : 32    31 : 30 | 42 : 36        97 : 66 | 123 : 81
+//     fp32 (T, 2047, 4095)   112 : 114 | 135 : 135    133 : 130 | 174 : 168    199 : 198 | 284 : 273    1224 : 1108 | 1725 : 1584
+// (Rows of a wider array and arrays that start elsewhere are not copied: the workspace's size does not depend on where they lie.)
 struct Workspace {
     int64_t ld_f, ld_c;            // elements of a row; ld_c 0: no copies
     int64_t grad, x, w;            // bytes of grad_gate (and of grad_up), of the copies of X and of a weight
@@ -69,10 +74,10 @@ int launched(int rc) { return rc == 0 ? CACNN_OK : CACNN_ERR_LAUNCH; }
 //     128 x 128, two of two stages           1.6             3.8
 //     256 x 256                              2.0             -
 //     64 x 128, three of two stages          -               1.0 for each tile of a compute unit, 1.3 for one
-// Examples, us, the chosen kernel first: 8 bits (64, 8192, 4096) 15 on 32 x 32, 22 on 64 x 32; (256, 4096, 4096) 15.5 on 64 x 64, 22 on 64 x 32; (1024, 4096, 4096)
-// 34 on 128 x 128 with four stages, 39 with two, 47 on 64 x 64; (2048, 4096, 4096) 51 with two stages, 64 with four, 78 on 256 x 256; bf16 gated (8192, 4096, 8192)
-// 972 on 256 x 256, 1135 on 128 x 128 with two stages; fp32 gated (1028, 6976, 3712) 874 on 64 x 128, 975 on 64 x 32, 1275 on 128 x 128, (6261, 2494, 912) through
-// registers 522, 630 and 631.
+// Examples, us, the chosen kernel first: 8 bits (64, 8192, 4096) 12 on 32 x 32, 16 on 64 x 32; (256, 4096, 4096) 14 on 64 x 64, 19 on 64 x 32; (1024, 4096, 4096)
+// 30 on 128 x 128 with four stages, 35 with two, 47 on 64 x 64; (2048, 4096, 4096) 42 with two stages, 54 with four, 53 on 256 x 256; bf16 gated (8192, 4096, 8192)
+// 952 on 256 x 256, 1139 on 128 x 128 with two stages; fp32 gated (1028, 6976, 3712) 863 on 64 x 128, 971 on 64 x 32, 1262 on 128 x 128, (6261, 2494, 912) through
+// registers 516, 630 and 627.
 int cacnn::matmul_kernel(const FeedArgs& a, int form, int dtype, bool direct) {
     const bool f32 = dtype == FEED_F32, gated = form == FEED_GATED;
     const double slabs = (double)a.q[0].k * feed_size(dtype) / 128 * a.segments, ahead = direct ? 1.0 : 1.7;

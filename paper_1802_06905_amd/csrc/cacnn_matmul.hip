@@ -5,21 +5,24 @@
 // as its first operand and 32 rows as its second, so a lane ends up with one row m and runs of four adjacent columns, which
 // leave in one store each, and the scale of a row in 8 bits is one number per lane.
 //
-// A workgroup owns BM x BN of Out and walks the contraction in slabs of 128 bytes a row, which are staged in LDS, two at a time.
-//   contraction contiguous ([row][k]): LDS keeps rows of 128 bytes; the 16-byte chunk c of row r lies at c ^ (r & 7), so that the eight lanes of
-//     an LDS access, eight rows at the same chunk, meet all banks once.  A lane's chunk holds the 8 (bf16), 4 (fp32) or 16 (8 bits)
+// A workgroup owns BM x BN of Out and walks the contraction in slabs of 128 bytes a row (bf16 on 256 x 256: 64), two or four of them in LDS or on their way.
+//   contraction contiguous ([row][k]): LDS keeps rows of a slab's length; the 16-byte chunk c of row r lies at c ^ ((r >> 1) & 7) (64 bytes: c ^ ((r >> 2) & 3)), so
+//     that the lanes of an LDS access, adjacent rows at the same chunk, spread over all banks (two, or four, rows are as wide as these).  A lane's chunk holds the 8 (bf16), 4 (fp32) or 16 (8 bits)
 //     contraction indices that it feeds to the matrix instructions; which index goes to which half of a wave does not matter, because
 //     both operands use the same assignment.
 //   contraction strided ([k][row]): LDS keeps the rows of k as they lie in memory, in blocks of 64 bytes (bf16, read by the
 //     transposing loads) or 128 (fp32, read word by word) that change places with k, for the same reason.
-// (The counter of LDS bank conflicts says 0, and LDS is read a fifth of the time.)
+// Counted on tiles of 256 x 256, bf16 (4096, 4096, 4096), gated and both gradients, and 8 bits (8192, 8192, 4096), and on fp32's of 128 x 128: bank conflicts
+// are 1 or 2 % of LDS's busy cycles, which are 21 to 25 % of all (fp32 7 to 11 %).
 //
-// What bounds large products is the chip's power and what is left between the matrix instructions: bf16 gated (4096, 4096, 4096), 0.27 TFLOP in 250 us,
-// keeps the matrix pipes busy for 54 % of the cycles at 1.94 GHz; (8192, 4096, 8192) takes 985 us with random data and 786 with zeros.  Measured:
-//     8 bits (8192, 8192, 4096)                       271 us, 2030 TFLOP/s (a library product of 8192 x 8192 x 8192 2670)
-//     bf16 gated (8192, 4096, 8192), three results    1005 us, 1095 TFLOP/s (1410);  its gradients, 8 T C F, 2050 us, 1070 TFLOP/s
-//     fp32 gated (1024, 2048, 2048)                   136 us, 126 TFLOP/s (151)
-// Few rows are bound by the weights' way from memory: one token bf16 (4096, 2 x 8192) 23.5 us on the device, 5.7 TB/s; in 8 bits (4096, 8192) 7.6 us, 4.4 TB/s.
+// What bounds large products is the chip's power and what is left between the matrix instructions: those calls keep the matrix pipes busy for 59 % (gated), 53 % (its
+// gradients) and 56 % (8 bits) of the cycles at 1.83 to 1.96 GHz, fp32 for 76 to 79 %; an earlier state of the bf16 kernel took 985 us for (8192, 4096, 8192) with
+// random data and 786 with zeros.  Measured (in brackets a library product of 8192 x 8192 x 8192 in the same process, its right operand transposed, as here):
+//     8 bits (8192, 8192, 4096)                       273 us one after another with other calls between, 252 alone, 2010 to 2180 TFLOP/s (3270)
+//     bf16 gated (8192, 4096, 8192), three results    1004 and 975 us, 1095 to 1130 TFLOP/s (1620);  its gradients, 8 T C F, 2050 us, 1070 TFLOP/s
+//     fp32 gated (1028, 6976, 3712)                   863 us, 123 TFLOP/s (154)
+// Few rows are bound by the weights' way: one token bf16 (4096, 2 x 8192) 31 us with weights from memory, 4.3 TB/s, 24 where the last call's are still in the last-level
+// cache; in 8 bits (4096, 8192) 10.3 and 7.5, 3.3 and 4.5 TB/s.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -673,8 +676,8 @@ __global__ void __launch_bounds__(WM* WN * 64, WM* WN == 4 ? 2 : 1) matmul_block
                 finish_run<DT, S::GATED, decltype(stream)::value>(a, at.product, m0 + (wm * QB + h) * 32 + row, n0 + block_of(0) * 32 + col, v, u);
             }
         };
-        // (whole lines past the L2: the 8-bit product of (8192, 8192, 4096) 281 -> 271 us.  A gated wave's are half lines: 1015 -> 1042; the gradients in
-        // bf16, four times the arithmetic to a line, gain nothing: 2024 -> 2038)
+        // (whole lines past the L2: the 8-bit product of (8192, 8192, 4096) 281 -> 271 us; with fp32 results (8192, 2048, 8192) 274 -> 268, (1024, 4096, 4096) 48.7 -> 47.4,
+        // (8192, 512, 8192) 96 either way.  A gated wave's are half lines: 1015 -> 1042; the gradients in bf16, four times the arithmetic to a line, gain nothing: 2024 -> 2038)
         constexpr bool STREAMS = ESZ == 1 && !S::GATED;
         if (STREAMS && a.out[at.product].lines) rows(std::integral_constant<bool, STREAMS>{});
         else rows(std::false_type{});
