@@ -275,6 +275,7 @@ int cacnn_pool_forward(const cacnn_problem* problem, int dtype, int mode, const 
  * another.  T may be 0 (nothing is written but weight gradients, which are zeros; pointers to arrays of T rows may then be NULL).
  * Limits: T <= 2^31 - 1, row lengths and strides <= 2^20, rows / 128 times columns / 64 of a result, each rounded up, < 2^24 (1.3e11 elements).
  * For a gated projection those of X's gradient and of both weights' together too, whichever results a call asks for.
+ * Operands whose rows start at multiples of 16 bytes, and are (C elements) whole ones, are the fastest: others take large products up to twice as long.
  * Pointers must be aligned to their element size; results must not overlap operands.  Accumulation is in fp32; a result in bf16 is rounded once,
  * to nearest even.  Every call adds up in a fixed order: the same call gives the same bits.  Calls enqueue on the stream and return; they never
  * synchronise, allocate nothing, keep no reference and may be captured into a graph.

@@ -106,7 +106,7 @@ _erfc = np.vectorize(math.erfc, otypes=[float])
 def activation_steps(name, g):
     """(act, how far its 32-bit steps may be, act', how far its may be), relative to the numbers that they multiply and add, so that a gate far below
     zero, whose act is small, has to be right in its leading digits too.  Counted: 2^-24 for a rounding or a constant's, an ulp for a power of two or a
-    reciprocal, 16 for the complementary error function, and what a relative error r of its argument y makes of e^y: |y| r."""
+    reciprocal, 16 for the tail of the normal distribution, and what a relative error r of its argument y makes of e^y: |y| r."""
     ulp, tiny = 2.0 ** -23, 2.0 ** -120
     if name == "gelu":
         share = 0.5 * _erfc(-g / math.sqrt(2))
